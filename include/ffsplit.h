@@ -66,7 +66,9 @@ enum { FFSPLIT_SCORE_SUMSQ = 0,   /* Eq. 3: ||sigma(X U[:,j])||_F^2 * ||V[j,:]||
  * The caller must not have used the workspace for anything else in between.            */
 #define FFSPLIT_SCORE_REUSE_TILED 0x100
 enum { FFSPLIT_WS_SCORE = 0, FFSPLIT_WS_SELECT = 1, FFSPLIT_WS_BUILD = 2, FFSPLIT_WS_FORWARD = 3,
-       FFSPLIT_WS_FACTORIZE = 4, FFSPLIT_WS_STACK = 5 };
+       FFSPLIT_WS_FACTORIZE = 4, FFSPLIT_WS_STACK = 5,
+       FFSPLIT_WS_DENSE_FORWARD = 6, FFSPLIT_WS_DENSE_BACKWARD = 7, FFSPLIT_WS_DENSE_STACK = 8,
+       FFSPLIT_WS_GRAD_NORM = 9 /* T: the number of tensors; desc may be NULL */ };
 
 enum { FFSPLIT_OK = 0,
        FFSPLIT_E_NULLPTR = -1,     /* a required pointer is NULL                          */
@@ -297,6 +299,115 @@ int ffsplit_stack_forward(const ffsplit_desc_t* desc, int32_t n_layers, const vo
                           const float* const* b1_packed, const float* const* b2,
                           float* x, int64_t T, float eps,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Training the layer that a split is cut from, or the heavy neurons that it keeps ----
+ *
+ * Sec. 5.1 fine-tunes after the split.  The calls below evaluate and differentiate a feed-forward layer
+ * whose weights lie as the caller's program has them (W1, Wg [d_model, d_ff], W2 [d_ff, d_model],
+ * row-major): an optimiser changes them every step, so nothing is packed.  The heavy part FFN_1 of a
+ * split is such a layer of k neurons (columns h2 of W1 and Wg, rows h2 of W2).
+ * Of the descriptor they read d_model (a multiple of 8), d_ff (any number), act and dtype; k, rem_kind,
+ * rank and group are ignored.  d_model and d_ff are below 2^20.  No buffer that a call writes may
+ * overlap another one of the call, but where it is said.
+ */
+
+/* Bytes of what ffsplit_dense_forward keeps for the backward pass (pure host arithmetic, never less for
+ * more tokens): H and the activation's derivatives, (1 + number of up projections) d_ff values a token. */
+size_t ffsplit_dense_kept_bytes(const ffsplit_desc_t* desc, int64_t T);
+
+/*
+ *   Y = [residual +] H W2,   H = gelu(X W1)   or   H = silu(X Wg) * (X W1).
+ * X [T, d_model]; Y [T, d_model] in desc->dtype, or fp32 if y_f32.  residual: NULL, or fp32
+ * [T, d_model]; may be the same buffer as Y when Y is fp32.  kept: NULL, or
+ * ffsplit_dense_kept_bytes(desc, T) bytes, 256-byte aligned, written for ffsplit_dense_backward (private
+ * layout).  Accumulation in fp32; H is rounded to desc->dtype between the two products, and so are the
+ * kept derivatives.  The activation's forms here: GeLU by the rational form 7.1.26 of Abramowitz and
+ * Stegun (absolute error of Phi below 1e-7) in bf16, erff in fp32.
+ * workspace: ffsplit_workspace_bytes(desc, FFSPLIT_WS_DENSE_FORWARD, T).
+ */
+int ffsplit_dense_forward(const ffsplit_desc_t* desc, const void* X, int64_t T,
+                          const void* W1, const void* Wg, const void* W2,
+                          void* Y, const float* residual, int32_t y_f32, void* kept,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Flags of the backward calls. */
+#define FFSPLIT_GRAD_F32 0x1          /* the weights' gradients are fp32 whatever desc->dtype          */
+#define FFSPLIT_GRAD_ACCUMULATE 0x2   /* they are added to what their buffers hold (micro-batches)     */
+
+/*
+ * Backward pass of ffsplit_dense_forward for the same X and weights and the `kept` that it wrote (which
+ * is only read, and may be used again).  With dH = dY W2^T:
+ *   SWIGLU  dU = dH * silu(Z), dG = dH * (X W1) * silu'(Z), Z = X Wg;
+ *           dX = dU W1^T + dG Wg^T;  dW1 = X^T dU;  dWg = X^T dG;  dW2 = H^T dY
+ *   GELU    dU = dH * gelu'(X W1);  dX = dU W1^T;  dW1 = X^T dU;  dW2 = H^T dY
+ * dY, dX [T, d_model] in desc->dtype; dW1, dWg, dW2 in the shape of their weights, in desc->dtype or fp32
+ * (FFSPLIT_GRAD_F32).  Any of dX, dW1, dWg, dW2 may be NULL and is then not computed; dWg must be NULL
+ * unless SWIGLU.  (The gradient of a residual is that of Y and is not formed here.)  dU and dG are
+ * rounded to desc->dtype; sums are fp32.  T = 0: the gradients are set to zero unless accumulated.
+ * workspace: ffsplit_workspace_bytes(desc, FFSPLIT_WS_DENSE_BACKWARD, T).
+ */
+int ffsplit_dense_backward(const ffsplit_desc_t* desc, const void* X, int64_t T,
+                           const void* W1, const void* Wg, const void* W2, const void* kept,
+                           const void* dY, void* dX, void* dW1, void* dWg, void* dW2, int32_t flags,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward pass of ffsplit_token_rmsnorm: with r = 1 / sqrt(mean(x^2) + eps) per token and dn the
+ * gradient of n(x) (in `dtype`),
+ *   dx = [residual +] r dn - x r^3 mean(x * dn).
+ * x, dx, residual fp32 [T, d_model]; residual (NULL: none) is the gradient that goes around the norm, and
+ * may be the same buffer as dx.  dx_cast: NULL, or [T, d_model] in `dtype`, receives dx as well (the
+ * gradient that the layer below takes).  All arithmetic in fp32.
+ */
+int ffsplit_token_rmsnorm_backward(const float* x, const void* dn, int64_t T, int32_t d_model, float eps,
+                                   int32_t dtype, const float* residual, float* dx, void* dx_cast, void* stream);
+
+/*
+ * Norm over all elements of n tensors, sqrt(sum g^2), to *norm (device).  grads, counts, dtypes: HOST
+ * arrays of n device pointers, element counts (0 is allowed, the pointer may then be NULL) and
+ * FFSPLIT_F32 / FFSPLIT_BF16.  Squares are formed and added in 64 bits.  *nonfinite (device, may be
+ * NULL): FFSPLIT_E_NONFINITE if the norm is not a finite fp32 number, else 0.
+ * workspace: ffsplit_workspace_bytes(NULL, FFSPLIT_WS_GRAD_NORM, n).
+ */
+int ffsplit_grad_norm(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                      float* norm, int32_t* nonfinite, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Clipping by that norm: out[i] = grads[i] * (max_norm / *norm) where *norm > max_norm; otherwise, and
+ * where *norm is not finite (the caller's program then skips the step), out[i] = grads[i] unchanged.
+ * out: HOST array of n device pointers in the types of grads; out[i] == grads[i] scales in place.
+ * The norm is read on the device: nothing waits.  max_norm > 0 (infinity: nothing is scaled).
+ */
+int ffsplit_grad_clip(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,
+                      const float* norm, float max_norm, void* const* out, void* stream);
+
+/* Bytes of what ffsplit_dense_stack_forward keeps for the backward pass. */
+size_t ffsplit_dense_stack_kept_bytes(const ffsplit_desc_t* desc, int32_t n_layers, int64_t T);
+
+/*
+ * The stack of ffsplit_stack_forward on uncompressed layers, x <- x + FFN_l(n(x)), for training.
+ * W1, Wg, W2: HOST arrays of n_layers device pointers (Wg NULL unless SWIGLU).  x [T, d_model] fp32, in
+ * place.  kept: NULL, or ffsplit_dense_stack_kept_bytes(...) bytes, 256-byte aligned.
+ * workspace: ffsplit_workspace_bytes(desc, FFSPLIT_WS_DENSE_STACK, T).
+ */
+int ffsplit_dense_stack_forward(const ffsplit_desc_t* desc, int32_t n_layers, const void* const* W1,
+                                const void* const* Wg, const void* const* W2, float* x, int64_t T, float eps,
+                                void* kept, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass.  dx [T, d_model] fp32: on entry the gradient of the stream behind the last layer, on
+ * return that of the stream in front of the first.  dW1, dWg, dW2: HOST arrays of n_layers device pointers
+ * that receive the weights' gradients (flags as for ffsplit_dense_backward).  If norm is not NULL the norm
+ * over all of them goes to *norm and *nonfinite (ffsplit_grad_norm; nonfinite may be NULL), and if also
+ * max_norm > 0 they are clipped in place (ffsplit_grad_clip).
+ * workspace: as for the forward pass.
+ */
+int ffsplit_dense_stack_backward(const ffsplit_desc_t* desc, int32_t n_layers, const void* const* W1,
+                                 const void* const* Wg, const void* const* W2, const void* kept, float* dx,
+                                 int64_t T, float eps, void* const* dW1, void* const* dWg, void* const* dW2,
+                                 int32_t flags, float max_norm, float* norm, int32_t* nonfinite,
+                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measured ceilings of the machine, for the benchmark's report (nothing on the

@@ -12,5 +12,8 @@ from .binding import (  # noqa: F401
     Desc, FFSplitError, lib, lib_path, status_string, make_desc,
     workspace_bytes, split_bytes, score_neurons, select_heavy, build_split, forward, split_export,
     factorize_remainder, select_heavy_static, SELECT_STATIC_MAX_DFF,
+    WS_DENSE_FORWARD, WS_DENSE_BACKWARD, WS_DENSE_STACK, WS_GRAD_NORM, GRAD_F32, GRAD_ACCUMULATE, E_NONFINITE,
+    dense_kept_bytes, dense_forward, dense_backward, token_rmsnorm_backward, grad_norm, grad_clip, clip_grad_norm,
+    dense_stack_forward, dense_stack_backward,
     probe_mfma, probe_stream_read, forward_ex, pack_neuron_bias, token_rmsnorm, stack_forward, Epilogue,
 )

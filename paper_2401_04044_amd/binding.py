@@ -10,6 +10,8 @@ REM_NONE, REM_DENSE, REM_LOWRANK, REM_INT4, REM_W3H8 = 0, 1, 2, 3, 4
 SCORE_SUMSQ, SCORE_MEAN_L2, SCORE_ACT_ONLY = 0, 1, 2
 SCORE_REUSE_TILED = 0x100
 WS_SCORE, WS_SELECT, WS_BUILD, WS_FORWARD, WS_FACTORIZE, WS_STACK = 0, 1, 2, 3, 4, 5
+WS_DENSE_FORWARD, WS_DENSE_BACKWARD, WS_DENSE_STACK, WS_GRAD_NORM = 6, 7, 8, 9
+GRAD_F32, GRAD_ACCUMULATE = 1, 2
 E_NONFINITE = -7
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -76,6 +78,26 @@ def _load():
     L.ffsplit_probe_stream_read.argtypes = [vp, sz, i32, vp, vp]
     L.ffsplit_factorize_remainder.restype = ctypes.c_int
     L.ffsplit_factorize_remainder.argtypes = [dp, vp, vp, vp, vp, ctypes.c_uint32, ctypes.POINTER(vp), vp, sz, vp]
+    vpp, f32 = ctypes.POINTER(vp), ctypes.c_float
+    L.ffsplit_dense_kept_bytes.restype = sz
+    L.ffsplit_dense_kept_bytes.argtypes = [dp, i64]
+    L.ffsplit_dense_forward.restype = ctypes.c_int
+    L.ffsplit_dense_forward.argtypes = [dp, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+    L.ffsplit_dense_backward.restype = ctypes.c_int
+    L.ffsplit_dense_backward.argtypes = [dp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    L.ffsplit_token_rmsnorm_backward.restype = ctypes.c_int
+    L.ffsplit_token_rmsnorm_backward.argtypes = [vp, vp, i64, i32, f32, i32, vp, vp, vp, vp]
+    L.ffsplit_grad_norm.restype = ctypes.c_int
+    L.ffsplit_grad_norm.argtypes = [i32, vpp, ctypes.POINTER(i64), ctypes.POINTER(i32), vp, vp, vp, sz, vp]
+    L.ffsplit_grad_clip.restype = ctypes.c_int
+    L.ffsplit_grad_clip.argtypes = [i32, vpp, ctypes.POINTER(i64), ctypes.POINTER(i32), vp, f32, vpp, vp]
+    L.ffsplit_dense_stack_kept_bytes.restype = sz
+    L.ffsplit_dense_stack_kept_bytes.argtypes = [dp, i32, i64]
+    L.ffsplit_dense_stack_forward.restype = ctypes.c_int
+    L.ffsplit_dense_stack_forward.argtypes = [dp, i32, vpp, vpp, vpp, vp, i64, f32, vp, vp, sz, vp]
+    L.ffsplit_dense_stack_backward.restype = ctypes.c_int
+    L.ffsplit_dense_stack_backward.argtypes = [dp, i32, vpp, vpp, vpp, vp, vp, i64, f32, vpp, vpp, vpp, i32, f32, vp, vp,
+                                               vp, sz, vp]
     L.ffsplit_split_export.restype = ctypes.c_int
     L.ffsplit_split_export.argtypes = [dp, vp, i32, vp, vp, vp]
     return L
@@ -270,6 +292,247 @@ def stack_forward(desc, splits, x, b1_packed=None, b2=None, eps=1e-6, workspace=
                                    ctypes.c_float(eps), _ptr(ws), ws.numel(), _stream())
     _check(rc, "ffsplit_stack_forward")
     return x
+
+
+_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
+
+
+def _take(t, what, shape, dtypes, device):
+    """A tensor argument of the training calls: they take plain row-major matrices, so that a view with
+    strides, another type or another device is an error here and not a wrong result there."""
+    if t is None:
+        return None
+    if not isinstance(dtypes, tuple):
+        dtypes = (dtypes,)
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what}: {t.dtype}, wanted {' or '.join(map(str, dtypes))}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, wanted {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: not contiguous")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, wanted {device}")
+    return t
+
+
+def _take_layer(desc, W1, Wg, W2, device, what=""):
+    dt, d, f = _DTYPES[desc.dtype], desc.d_model, desc.d_ff
+    _take(W1, "W1" + what, (d, f), dt, device)
+    _take(Wg, "Wg" + what, (d, f), dt, device)
+    _take(W2, "W2" + what, (f, d), dt, device)
+
+
+def _scratch(nbytes, workspace, device):
+    if workspace is not None:
+        return _take(workspace, "workspace", None, torch.uint8, device)
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def _ptrs(ts):
+    if ts is None:
+        return None
+    a = (ctypes.c_void_p * max(len(ts), 1))()
+    for i, t in enumerate(ts):
+        a[i] = None if t is None else t.data_ptr()
+    return a
+
+
+def dense_kept_bytes(desc, T):
+    return int(lib.ffsplit_dense_kept_bytes(ctypes.byref(desc), T))
+
+
+def dense_forward(desc, X, W1, Wg, W2, Y=None, residual=None, y_f32=False, want_saved=False, saved=None, workspace=None):
+    """The uncompressed layer on plain weights: Y = [residual +] act(X W1, X Wg) W2.  Returns Y, or (Y, saved)
+    with want_saved or a buffer for it: what dense_backward needs."""
+    T, dev, dt = X.shape[0], X.device, _DTYPES[desc.dtype]
+    _take(X, "X", (T, desc.d_model), dt, dev)
+    _take_layer(desc, W1, Wg, W2, dev)
+    y_dt = torch.float32 if y_f32 else dt
+    if Y is None:
+        Y = torch.empty((T, desc.d_model), dtype=y_dt, device=dev)
+    _take(Y, "Y", (T, desc.d_model), y_dt, dev)
+    _take(residual, "residual", (T, desc.d_model), torch.float32, dev)
+    keep = want_saved or saved is not None
+    if keep:
+        need = dense_kept_bytes(desc, T)
+        if saved is None:
+            saved = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _take_kept(saved, need, dev)
+    with torch.cuda.device(dev):
+        ws = _scratch(workspace_bytes(desc, WS_DENSE_FORWARD, T), workspace, dev)
+        rc = lib.ffsplit_dense_forward(ctypes.byref(desc), _ptr(X), T, _ptr(W1), _ptr(Wg), _ptr(W2), _ptr(Y), _ptr(residual),
+                                       1 if y_f32 else 0, _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _stream())
+    _check(rc, "ffsplit_dense_forward")
+    return (Y, saved) if keep else Y
+
+
+def _take_kept(saved, need, device):
+    _take(saved, "saved", None, torch.uint8, device)
+    if saved.numel() < need:
+        raise ValueError(f"saved: {saved.numel()} bytes, wanted {need}")
+
+
+def _grad_flags(accumulate, grad_f32):
+    return (GRAD_ACCUMULATE if accumulate else 0) | (GRAD_F32 if grad_f32 else 0)
+
+
+def _grads_for(desc, grads, accumulate, grad_f32, device, what=""):
+    """The gradients' buffers of one layer: given ones (a dict; a missing or None entry is not computed), or new."""
+    names = ("W1", "Wg", "W2") if desc.act == ACT_SWIGLU else ("W1", "W2")
+    dt = torch.float32 if grad_f32 else _DTYPES[desc.dtype]
+    shapes = {"W1": (desc.d_model, desc.d_ff), "Wg": (desc.d_model, desc.d_ff), "W2": (desc.d_ff, desc.d_model)}
+    if grads is None:
+        if accumulate:
+            raise ValueError("accumulate: the gradients to add to are wanted")
+        return {k: torch.empty(shapes[k], dtype=dt, device=device) if k in names else None for k in shapes}
+    for k, g in grads.items():
+        if k not in shapes or (g is not None and k not in names):
+            raise ValueError(f"no gradient {k!r} of this layer")
+        _take(g, f"gradient of {k}{what}", shapes[k], dt, device)
+    return {k: grads.get(k) for k in shapes}
+
+
+def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=None, accumulate=False, grad_f32=False,
+                   workspace=None):
+    """Backward pass of dense_forward.  Returns (dX or None, {"W1", "Wg", "W2": gradients or None})."""
+    T, dev, dt = X.shape[0], X.device, _DTYPES[desc.dtype]
+    _take(X, "X", (T, desc.d_model), dt, dev)
+    _take_layer(desc, W1, Wg, W2, dev)
+    _take(dY, "dY", (T, desc.d_model), dt, dev)
+    _take_kept(saved, dense_kept_bytes(desc, T), dev)
+    if dX is None and want_dx:
+        dX = torch.empty((T, desc.d_model), dtype=dt, device=dev)
+    _take(dX, "dX", (T, desc.d_model), dt, dev)
+    g = _grads_for(desc, grads, accumulate, grad_f32, dev)
+    with torch.cuda.device(dev):
+        ws = _scratch(workspace_bytes(desc, WS_DENSE_BACKWARD, T), workspace, dev)
+        rc = lib.ffsplit_dense_backward(ctypes.byref(desc), _ptr(X), T, _ptr(W1), _ptr(Wg), _ptr(W2), _ptr(saved), _ptr(dY),
+                                        _ptr(dX), _ptr(g["W1"]), _ptr(g["Wg"]), _ptr(g["W2"]),
+                                        _grad_flags(accumulate, grad_f32), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "ffsplit_dense_backward")
+    return dX, g
+
+
+def token_rmsnorm_backward(x, dn, eps=1e-6, residual=None, dx=None, want_cast=False):
+    """Gradient of x behind token_rmsnorm: dx = [residual +] r dn - x r^3 mean(x dn), fp32 [T, d] (residual may
+    be dx).  Returns dx, or (dx, dx in dn's type) with want_cast."""
+    T, d = x.shape
+    dev = x.device
+    _take(x, "x", (T, d), torch.float32, dev)
+    _take(dn, "dn", (T, d), (torch.float32, torch.bfloat16), dev)
+    _take(residual, "residual", (T, d), torch.float32, dev)
+    if dx is None:
+        dx = torch.empty_like(x)
+    _take(dx, "dx", (T, d), torch.float32, dev)
+    cast = torch.empty_like(dn) if want_cast else None
+    with torch.cuda.device(dev):
+        rc = lib.ffsplit_token_rmsnorm_backward(_ptr(x), _ptr(dn), T, d, ctypes.c_float(eps),
+                                                BF16 if dn.dtype == torch.bfloat16 else F32, _ptr(residual), _ptr(dx),
+                                                _ptr(cast), _stream())
+    _check(rc, "ffsplit_token_rmsnorm_backward")
+    return (dx, cast) if want_cast else dx
+
+
+def _grad_list(grads, what="gradients"):
+    n = len(grads)
+    dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    counts, dtypes = (ctypes.c_int64 * max(n, 1))(), (ctypes.c_int32 * max(n, 1))()
+    for i, g in enumerate(grads):
+        _take(g, what, None, (torch.float32, torch.bfloat16), dev)
+        counts[i] = g.numel()
+        dtypes[i] = F32 if g.dtype == torch.float32 else BF16
+    return n, dev, counts, dtypes
+
+
+def grad_norm(grads, norm=None, flag=None, workspace=None):
+    """Norm over all elements of all tensors.  Returns (norm [1] fp32, flag [1] int32), on the device; the flag is
+    E_NONFINITE if the norm is not finite, else 0."""
+    n, dev, counts, dtypes = _grad_list(grads)
+    with torch.cuda.device(dev):
+        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else _take(norm, "norm", (1,), torch.float32, dev)
+        flag = torch.empty(1, dtype=torch.int32, device=dev) if flag is None else _take(flag, "flag", (1,), torch.int32, dev)
+        ws = _scratch(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, n), workspace, dev)
+        rc = lib.ffsplit_grad_norm(n, _ptrs(grads), counts, dtypes, _ptr(norm), _ptr(flag), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "ffsplit_grad_norm")
+    return norm, flag
+
+
+def grad_clip(grads, norm, max_norm, out=None):
+    """out = grads * min(1, max_norm / norm), in place without `out`; unchanged where the norm (on the device) is
+    not finite.  Returns the list of clipped gradients."""
+    n, dev, counts, dtypes = _grad_list(grads)
+    out = grads if out is None else out
+    if len(out) != n:
+        raise ValueError(f"out: {len(out)} tensors for {n} gradients")
+    for g, o in zip(grads, out):
+        _take(o, "out", g.shape, g.dtype, dev)
+    _take(norm, "norm", (1,), torch.float32, dev)
+    with torch.cuda.device(dev):
+        rc = lib.ffsplit_grad_clip(n, _ptrs(grads), counts, dtypes, _ptr(norm), ctypes.c_float(max_norm), _ptrs(out),
+                                   _stream())
+    _check(rc, "ffsplit_grad_clip")
+    return out
+
+
+def clip_grad_norm(grads, max_norm, out=None, workspace=None):
+    """grad_norm, then grad_clip.  Returns (norm, flag, clipped gradients)."""
+    norm, flag = grad_norm(grads, workspace=workspace)
+    return norm, flag, grad_clip(grads, norm, max_norm, out)
+
+
+def _stack_args(desc, layers, device):
+    for l, W in enumerate(layers):
+        _take_layer(desc, W["W1"], W.get("Wg"), W["W2"], device, f" of layer {l}")
+    gated = desc.act == ACT_SWIGLU
+    return (_ptrs([W["W1"] for W in layers]), _ptrs([W.get("Wg") for W in layers]) if gated else None,
+            _ptrs([W["W2"] for W in layers]))
+
+
+def dense_stack_forward(desc, layers, x, eps=1e-6, want_saved=False, saved=None, workspace=None):
+    """x <- x + FFN_l(n(x)) for every layer (dicts W1, Wg, W2), in place on the fp32 stream x [T, d].  Returns x, or
+    what dense_stack_backward needs with want_saved or a buffer for it."""
+    n, T, dev = len(layers), x.shape[0], x.device
+    _take(x, "x", (T, desc.d_model), torch.float32, dev)
+    keep = want_saved or saved is not None
+    if keep:
+        need = int(lib.ffsplit_dense_stack_kept_bytes(ctypes.byref(desc), n, T))
+        if saved is None:
+            saved = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        _take_kept(saved, need, dev)
+    W1, Wg, W2 = _stack_args(desc, layers, dev)
+    with torch.cuda.device(dev):
+        ws = _scratch(workspace_bytes(desc, WS_DENSE_STACK, T), workspace, dev)
+        rc = lib.ffsplit_dense_stack_forward(ctypes.byref(desc), n, W1, Wg, W2, _ptr(x), T, ctypes.c_float(eps),
+                                             _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _stream())
+    _check(rc, "ffsplit_dense_stack_forward")
+    return saved if keep else x
+
+
+def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumulate=False, grad_f32=False, max_norm=0.0,
+                         workspace=None):
+    """Backward pass of dense_stack_forward, in place on the stream's gradient dx [T, d].  Returns (gradients: a dict
+    W1, Wg, W2 per layer; their norm [1]; its flag [1]); with max_norm > 0 the gradients are clipped."""
+    n, T, dev = len(layers), dx.shape[0], dx.device
+    _take(dx, "dx", (T, desc.d_model), torch.float32, dev)
+    _take_kept(saved, int(lib.ffsplit_dense_stack_kept_bytes(ctypes.byref(desc), n, T)), dev)
+    if grads is not None and len(grads) != n:
+        raise ValueError(f"gradients of {len(grads)} layers for {n}")
+    g = [_grads_for(desc, grads[l] if grads is not None else None, accumulate, grad_f32, dev, f" of layer {l}")
+         for l in range(n)]
+    W1, Wg, W2 = _stack_args(desc, layers, dev)
+    gated = desc.act == ACT_SWIGLU
+    with torch.cuda.device(dev):
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        flag = torch.empty(1, dtype=torch.int32, device=dev)
+        need = max(workspace_bytes(desc, WS_DENSE_STACK, T), int(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, 3 * n)))
+        ws = _scratch(need, workspace, dev)
+        rc = lib.ffsplit_dense_stack_backward(ctypes.byref(desc), n, W1, Wg, W2, _ptr(saved), _ptr(dx), T,
+                                              ctypes.c_float(eps), _ptrs([q["W1"] for q in g]),
+                                              _ptrs([q["Wg"] for q in g]) if gated else None, _ptrs([q["W2"] for q in g]),
+                                              _grad_flags(accumulate, grad_f32), ctypes.c_float(max_norm), _ptr(norm),
+                                              _ptr(flag), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "ffsplit_dense_stack_backward")
+    return g, norm, flag
 
 
 def probe_mfma(workgroups, iters, scratch):

@@ -6,6 +6,7 @@
 #include "int4.h"
 #include "quant.h"
 #include "factor.h"
+#include "train.h"
 
 using namespace ffsplit;
 
@@ -192,6 +193,7 @@ size_t ffsplit_split_bytes(const ffsplit_desc_t* d) {
 
 size_t ffsplit_workspace_bytes(const ffsplit_desc_t* d, int32_t call_id, int64_t T) {
   if (call_id == FFSPLIT_WS_SELECT) return d ? select_workspace_bytes(d->d_ff) : 0;
+  if (call_id >= FFSPLIT_WS_DENSE_FORWARD) return train_workspace_bytes(d, call_id, T);
   if (check_desc(d, call_id != FFSPLIT_WS_SCORE) != FFSPLIT_OK || T < 0) return 0;
   const size_t esz = d->dtype == FFSPLIT_BF16 ? 2 : 4;
   if (call_id == FFSPLIT_WS_SCORE) {

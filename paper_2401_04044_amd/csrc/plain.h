@@ -1,0 +1,58 @@
+// Internal: products of the training path on plain row-major matrices (plain.hip), and what their
+// launches store.
+#pragma once
+#include "common.h"
+
+namespace ffsplit {
+
+// What a product does with its sums (Z, U: sums of the gate and up columns, S: of the only ones):
+//   EPI_OUT   C = S [+ resid] [+ C], in the storage type or fp32
+//   EPI_GLU   H = silu(Z) U, and if D1 is set D1 = dH/dU = silu(Z), D2 = dH/dZ = U silu'(Z)
+//   EPI_GELU  H = gelu(S), and if D1 is set D1 = gelu'(S)
+//   EPI_GRAD  O1 = S * D1 and, with D2, O2 = S * D2
+// H, D1, D2, O1, O2 have rows of ldi elements and n_store >= N stored columns; those from N on are
+// stored as zeros, so that a later reduction over them in whole 16-byte chunks adds nothing.
+enum { EPI_OUT = 0, EPI_GLU = 1, EPI_GELU = 2, EPI_GRAD = 3 };
+
+// D[m, n] = sum_k A(m, k) B(n, k), fp32 accumulation.  An operand is stored with its reduction
+// contiguous ("kc": element (r, k) at r * ld + k) or its rows ("mc": at k * ld + r).  ld a multiple of
+// 8, pointers 16-byte aligned; kc: the elements from K to the next multiple of 8 are zero in at least
+// one operand and finite in the other.
+struct PlainArgs {
+  const void* A[2];
+  const void* B[2];
+  int64_t lda, ldb;
+  int64_t a_bytes, b_bytes;   // of each: nothing at or beyond is read
+  int a_mc, b_mc;
+  int M, N, K;
+  // How the second operands take part:
+  //   segs = 2   the reduction goes over A[0] B[0] and then A[1] B[1], K elements each
+  //   twin       a second product A[0] B[1] beside the first, with its own destination C[1]
+  //   EPI_GLU    B[0] gate columns, B[1] up columns, summed in the same tile
+  int segs, twin;
+  void* C[2];
+  int64_t ldc;
+  int out_f32, accumulate;
+  const float* resid;
+  const void* D1;
+  const void* D2;
+  void* O1;
+  void* O2;
+  void* H;
+  int64_t ldi;
+  int n_store;
+  // The reduction cut into n_split ranges: fp32 sums [range][plane][M][ldp] that plain_reduce adds
+  // (plane 1: up columns, or the twin product)
+  float* part;
+  int n_split, ldp;
+  int group_m;   // row tiles per rasterisation group (set by the launcher)
+};
+
+// Bytes of scratch that hold the ranges' sums of any product (see plain_plan).
+size_t plain_part_room();
+// part: that many bytes
+int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st);
+// dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind; cols8 = cols rounded up to 8
+int launch_pad_rows(const void* src, void* dst, int64_t rows, int cols, int bf16, hipStream_t st);
+
+}  // namespace ffsplit

@@ -1,0 +1,445 @@
+// Products on plain row-major matrices in any orientation, with the store steps of the training path
+// (plain.h), gfx950 only.
+//
+//   D[M, N] = sum_k A(m, k) B(n, k)
+//
+// A layer's forward and backward pass read the same matrices along different axes (X W1, dY W2^T,
+// X^T dU, ...), and its weights change every step: a copy re-tiled for each use would cost 10 to 20 %
+// of the products' time.  So one kernel takes each operand as it lies in memory:
+//   kc: reduction contiguous.  A slab of 64 bytes per row; the 16-byte chunk c of row r sits in LDS at
+//       4 r + (c ^ f(r / 4)), f = 0 2 3 1: the four lane groups that a 16-byte LDS read serves at a time
+//       (lanes 0-3, 12-15, 20-27 and so on) then fall into different banks.
+//   mc: rows contiguous.  bf16 fragments are turned round on the way out of LDS (ds_read_b64_tr_b16:
+//       lane j of 16 gets column j of four 16-column rows), fp32 ones are read element by element.
+//       The LDS rows' pieces are exchanged by an XOR with the row number, so that the eight rows read
+//       at a time fall into different banks.
+// Both go from global memory straight into a ring of LDS stages (buffer loads with LDS destination).
+// The buffers' bounds are exact: what lies behind an operand's end reads as zero, which is how a
+// reduction that ends inside a slab and rows behind the last are handled, without masks in the loop.
+#include "plain_epi.h"
+#include <atomic>
+#include <algorithm>
+#include <math.h>
+#include <type_traits>
+
+namespace ffsplit {
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t* lfrag_t;
+
+union Frag {
+  u32x4_t u;
+  u32x2_t h[2];
+  bf16x8_t v;
+  f32x4_t f;
+};
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
+}
+__device__ __forceinline__ void wait_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+// workgroup barrier without a memory fence (the kernel orders its loads with explicit counters)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+__device__ __forceinline__ int xcd_remap(int i, int total) {
+  const int q = total >> 3, rem = total & 7, x = i & 7;
+  return x * q + (x < rem ? x : rem) + (i >> 3);
+}
+// swap the odd 16-lane rows of a with the even ones of b
+__device__ __forceinline__ void swap16(float& a, float& b) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ uint32_t kc_swizzle(uint32_t r4) { return (0x78u >> (2 * (r4 & 3))) & 3; }   // 0 2 3 1
+
+// bytes behind the offset `at` of a buffer of `bytes`, within what a resource's bound can say; uniform
+__device__ __forceinline__ int bytes_left(int64_t bytes, int64_t at) {
+  const int64_t left = bytes - at;
+  const int hi = __builtin_amdgcn_readfirstlane((int)(left >> 31)), lo = __builtin_amdgcn_readfirstlane((int)left);
+  return hi > 0 ? 0x7fffffff : hi < 0 ? 0 : lo;
+}
+// (the resource is built in scalar registers; the builtin returns a signed int)
+__device__ __forceinline__ const char* uniform(const char* q) {
+  const uint64_t u = (uint64_t)q;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+  return (const char*)(((uint64_t)hi << 32) | (uint64_t)lo);
+}
+constexpr uint32_t NOWHERE = 0x80000000u;   // beyond every bound
+// 16 bytes per lane from base + offset (zeros beyond `bytes`) straight into LDS, lane l to dst + 16 l.
+// base, bytes and dst in scalar registers.  In assembly because the compiler, when it sees a load into
+// LDS, waits for all of them before every turned-round LDS read; here the counts are kept by hand.  (The
+// first s_nop covers scalar registers just written by v_readfirstlane, the second m0.)
+__device__ __forceinline__ void load_to_lds(const char* base, int bytes, uint32_t dst, uint32_t offset) {
+  const uint64_t b = (uint64_t)base;
+  const u32x4_t r = {(uint32_t)b, (uint32_t)(b >> 32), (uint32_t)bytes, 0x00027000u};
+  asm volatile("s_nop 4\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(offset), "s"(r), "s"(dst)
+               : "memory");   // (m0: nothing else in these kernels uses it)
+}
+__device__ __forceinline__ uint32_t lds_offset(const char* q) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)q;
+}
+
+// One operand's side of the tile: R rows, in LDS at byte `region` of a stage.
+// Blocks of 1 KiB, one load instruction each: kc 16 rows x 64 bytes; mc 1024 / P k-rows x P bytes, P the
+// length of an LDS row (256 bytes, or the whole side if that is shorter).
+template <typename T, int R, bool MC>
+struct Side {
+  static constexpr int EPC = 16 / sizeof(T);          // elements per 16-byte chunk
+  static constexpr int BK = 4 * EPC;                  // depth of a slab
+  static constexpr int P = R * (int)sizeof(T) < 256 ? R * (int)sizeof(T) : 256;
+  static constexpr int SUB = P / (int)sizeof(T);      // mc: rows of the operand in one sub-block
+  static constexpr int KPB = 1024 / P;                // mc: k-rows of one load
+  static constexpr int BPS = BK / KPB;                // mc: loads of one sub-block
+  static constexpr int BLOCKS = R / 16;
+  static_assert(P == 256 || P == 128, "the exchange of pieces is written for these");
+
+  // mc: XOR on the chunk number within LDS row k.  bf16: a read serves rows 8 g + 0..3 of two groups g
+  // with 32 bytes of each; fp32: rows 4 g + t of four groups with 64 bytes.
+  static __device__ __forceinline__ uint32_t mc_swizzle(uint32_t k) {
+    if (sizeof(T) == 2) {
+      if (P == 256) return 2 * ((k & 3) + 4 * ((k >> 3) & 1));
+      return 2 * (((k >> 1) & 1) + 2 * ((k >> 3) & 1));
+    }
+    if (P == 256) return 4 * ((k >> 2) & 3);
+    return 4 * ((k >> 2) & 1);
+  }
+  // byte offset of the lane's 16 bytes of block b from the tile's first element, and (kc) its chunk
+  static __device__ __forceinline__ uint32_t source(int b, int lane, uint32_t ld, uint32_t* chunk) {
+    if (!MC) {
+      const uint32_t r = lane >> 2, c = (lane & 3) ^ kc_swizzle(r >> 2);
+      *chunk = c;
+      return ((uint32_t)b * 16 + r) * ld * (uint32_t)sizeof(T) + c * 16;
+    }
+    constexpr int CPR = P / 16;   // chunks of an LDS row
+    const uint32_t sub = b / BPS, k = (b % BPS) * KPB + lane / CPR;
+    const uint32_t c = (lane % CPR) ^ mc_swizzle(k);
+    *chunk = 0;
+    return k * ld * (uint32_t)sizeof(T) + sub * P + c * 16;
+  }
+  // the lane's part of a fragment address: rows l & 15 of a 16-row tile, elements 8 (l >> 4) .. + 7
+  // (fp32: 4 (l >> 4) .. + 3) of the slab
+  static __device__ __forceinline__ uint32_t lane_part(int lane) {
+    const uint32_t g = lane >> 4, j = lane & 15;
+    if (!MC) return j * 64 + ((g ^ kc_swizzle(j >> 2)) * 16);
+    if (sizeof(T) == 2) {
+      const uint32_t k = 8 * g + (j >> 2);
+      return k * P + ((((j & 3) >> 1) ^ mc_swizzle(k)) * 16) + (j & 1) * 8;
+    }
+    const uint32_t k = 4 * g;
+    return k * P + (((j >> 2) ^ mc_swizzle(k)) * 16) + (j & 3) * 4;
+  }
+  // fragment of the 16-row tile x of this side
+  static __device__ __forceinline__ void read(Frag& f, char* region, uint32_t lane, int x) {
+    if (!MC) {
+      f.u = *(const u32x4_t*)(region + x * 1024 + lane);
+      return;
+    }
+    constexpr int TPS = SUB / 16;
+    constexpr uint32_t TB = 16 * sizeof(T);     // bytes of a tile's piece of an LDS row
+    char* const at = region + (x / TPS) * (BK * P) + (lane ^ ((uint32_t)(x % TPS) * TB));
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lfrag_t)(at + u * 4 * P)));
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f.f[t] = *(const float*)(at + t * P);
+    }
+  }
+};
+
+template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, bool AMC, bool BMC, int EPI>
+__global__ void __launch_bounds__(WGM* WGN * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+plain_kernel(const PlainArgs p) {
+  constexpr bool PAIR = EPI == EPI_GLU;
+  constexpr int NW = WGM * WGN;
+  constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
+  constexpr int BNH = PAIR ? BN / 2 : BN;      // output columns of the tile
+  using SA = Side<T, BM, AMC>;
+  using SB = Side<T, BNH, BMC>;
+  constexpr int BK = SA::BK;
+  constexpr int A_BLK = BM / 16, B_BLK = BN / 16, HB = BNH / 16;   // HB: blocks of one matrix's columns
+  constexpr int LA = A_BLK / NW, LB = B_BLK / NW, LPW = LA + LB;
+  constexpr int STAGE = (A_BLK + B_BLK) * 1024;
+  static_assert(A_BLK % NW == 0 && B_BLK % NW == 0, "blocks divide over the wavefronts");
+  static_assert(!PAIR || HB % NW == 0 || NW % HB == 0, "a load belongs to one matrix");
+  static_assert(STAGES >= 2 && STAGES <= 5 && STAGES * LPW <= 63, "loads in flight must fit the counter");
+  static_assert(TM % 2 == 0 && (!PAIR || TN % 2 == 0), "row tiles are stored in pairs");
+
+  extern __shared__ u32x4_t smem_v[];
+  char* const smem = (char*)smem_v;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  const int tiles_n1 = (p.n_store + BNH - 1) / BNH, tiles_n = p.twin ? 2 * tiles_n1 : tiles_n1;
+  const int tiles_m = (p.M + BM - 1) / BM;
+  const int logical = xcd_remap(blockIdx.x, tiles_m * tiles_n);
+  const int gsz = p.group_m * tiles_n;
+  const int first_m = (logical / gsz) * p.group_m;
+  const int gm = min(tiles_m - first_m, p.group_m);
+  const int tm = first_m + (logical % gsz) % gm, tn2 = (logical % gsz) / gm;
+  const int which = tn2 >= tiles_n1, tn = which ? tn2 - tiles_n1 : tn2;
+  const int m0 = tm * BM, n0 = tn * BNH;
+
+  // slabs: segs times ceil(K / BK); this range's part of them
+  const int ns = (p.K + BK - 1) / BK;
+  const int total = ns * p.segs;
+  const int per = (total + p.n_split - 1) / p.n_split;
+  const int s0 = blockIdx.y * per;
+  const int nk = max(0, min(total, s0 + per) - s0);
+  const int k_end = (p.K + SA::EPC - 1) / SA::EPC * SA::EPC;   // kc: chunks from here on read as zero
+
+  uint32_t va[LA], vb[LB], ca = 0, cb = 0;
+#pragma unroll
+  for (int i = 0; i < LA; ++i) va[i] = SA::source(wave + i * NW, lane, (uint32_t)p.lda, &ca);
+#pragma unroll
+  for (int i = 0; i < LB; ++i) vb[i] = SB::source((wave + i * NW) % HB, lane, (uint32_t)p.ldb, &cb);
+  const int64_t a_org = (AMC ? (int64_t)m0 : (int64_t)m0 * p.lda) * (int)sizeof(T);
+  const int64_t b_org = (BMC ? (int64_t)n0 : (int64_t)n0 * p.ldb) * (int)sizeof(T);
+  const int64_t a_step = AMC ? (int64_t)BK * p.lda * (int)sizeof(T) : 64, b_step = BMC ? (int64_t)BK * p.ldb * (int)sizeof(T) : 64;
+
+  // all loads of slab s0 + rel into a stage
+  auto issue = [&](int rel, int stage) {
+    int s = s0 + rel, seg = 0;
+    if (s >= ns) { s -= ns; seg = 1; }   // (segs = 2)
+    const int64_t ao = a_org + s * a_step, bo = b_org + s * b_step;
+    const char* const a0 = uniform((const char*)(seg ? p.A[1] : p.A[0]) + ao);
+    const char* const b0 = uniform((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo);
+    const char* const b1 = PAIR ? uniform((const char*)p.B[1] + bo) : b0;
+    const int al = bytes_left(p.a_bytes, ao), bl = bytes_left(p.b_bytes, bo);
+    const bool a_out = !AMC && s * BK + (int)ca * SA::EPC >= k_end, b_out = !BMC && s * BK + (int)cb * SA::EPC >= k_end;
+    const uint32_t st = lds_offset(smem) + stage * STAGE;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) load_to_lds(a0, al, st + (wave + i * NW) * 1024, a_out ? NOWHERE : va[i]);
+#pragma unroll
+    for (int i = 0; i < LB; ++i)
+      load_to_lds(PAIR && (wave + i * NW) >= HB ? b1 : b0, bl, st + (A_BLK + wave + i * NW) * 1024, b_out ? NOWHERE : vb[i]);
+  };
+
+  f32x4_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  const uint32_t la = SA::lane_part(lane), lb = SB::lane_part(lane);
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < nk) issue(s, s);
+  int stage = 0;
+  for (int s = 0; s < nk; ++s) {
+    const int later = min(STAGES - 2, nk - 1 - s);   // younger slabs that may still be in flight
+    if (later <= 0) wait_vmcnt<0>();
+    else if (later == 1) wait_vmcnt<LPW>();
+    else if (later == 2) wait_vmcnt<2 * LPW>();
+    else wait_vmcnt<3 * LPW>();
+    wait_lgkmcnt0();
+    lds_barrier();   // slab s is there for all; all are done with slab s - 1
+    if (s + STAGES - 1 < nk) issue(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+    char* const st = smem + stage * STAGE;
+    Frag fa[TM], fb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int half = PAIR ? j / (TN / 2) : 0, jj = PAIR ? j % (TN / 2) : j;
+      // (the column tiles of a wavefront lie within one sub-block or are whole ones)
+      SB::read(fb[j], st + A_BLK * 1024 + half * HB * 1024, lb, wn * (PAIR ? TN / 2 : TN) + jj);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) SA::read(fa[i], st, la, wm * TM + i);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        if constexpr (sizeof(T) == 2) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j].v, fa[i].v, acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j].f[t], fa[i].f[t], acc[i][j], 0, 0, 0);
+        }
+      }
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+  }
+
+  // Store.  A lane holds columns 4 (l >> 4) .. + 3 of row l & 15 of each tile; exchanging lane rows
+  // between two row tiles leaves eight columns 8 (l >> 5) .. + 7 of row l & 31.
+#pragma unroll
+  for (int jj = 0; jj < (PAIR ? TN / 2 : TN); ++jj) {
+    const int col = n0 + wn * (PAIR ? WN / 2 : WN) + jj * 16 + 8 * (lane >> 5);
+#pragma unroll
+    for (int ip = 0; ip < TM; ip += 2) {
+      const int64_t row = m0 + wm * WM + ip * 16 + (lane & 31);
+      float v[8], u[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = acc[ip][jj][e]; v[4 + e] = acc[ip + 1][jj][e];
+        swap16(v[e], v[4 + e]);
+        if (PAIR) {
+          u[e] = acc[ip][jj + TN / 2][e]; u[4 + e] = acc[ip + 1][jj + TN / 2][e];
+          swap16(u[e], u[4 + e]);
+        }
+      }
+      if (row >= p.M || col >= p.n_store) continue;
+      if (p.part != nullptr) {
+        const int planes = PAIR || p.twin ? 2 : 1;
+        const int64_t at = (((int64_t)blockIdx.y * planes + which) * p.M + row) * p.ldp + col;
+        store8<float>(p.part, at, v);
+        if (PAIR) store8<float>(p.part, at + (int64_t)p.M * p.ldp, u);
+        continue;
+      }
+      emit8<T, EPI>(p, which, row, col, v, u);
+    }
+  }
+}
+
+// Sum of the ranges' fp32 sums in range order, and the store step.  One thread per row, plane of a twin
+// product and eight columns.
+template <typename T, int EPI>
+__global__ void __launch_bounds__(256) plain_reduce_kernel(const PlainArgs p) {
+  const int cpr = (p.n_store + 7) / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t per_plane = (int64_t)p.M * cpr;
+  const int which = p.twin && id >= per_plane;
+  const int64_t in = which ? id - per_plane : id;
+  if (in >= per_plane) return;
+  const int64_t row = in / cpr;
+  const int col = (int)(in % cpr) * 8;
+  const int planes = EPI == EPI_GLU || p.twin ? 2 : 1;
+  const int64_t plane = (int64_t)p.M * p.ldp;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int s = 0; s < p.n_split; ++s) {
+    const int64_t at = ((int64_t)s * planes + which) * plane + row * p.ldp + col;
+    float w[8];
+    load8<float>(p.part, at, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+    if (EPI == EPI_GLU) {
+      load8<float>(p.part, at + plane, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] += w[e];
+    }
+  }
+  emit8<T, EPI>(p, which, row, col, v, u);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src, T* dst, int64_t rows, int cols, int cols8) {
+  const int64_t n = rows * cols8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / cols8;
+    const int c = (int)(i % cols8);
+    dst[i] = c < cols ? src[r * cols + c] : (T)0;
+  }
+}
+
+template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, bool AMC, bool BMC, int EPI>
+static int launch_tile(const PlainArgs& a, hipStream_t st) {
+  constexpr size_t lds = (size_t)STAGES * (BM + BN) * 64;
+  static_assert(lds <= 160 * 1024, "LDS budget of a CU");
+  auto kern = plain_kernel<T, BM, BN, WGM, WGN, STAGES, AMC, BMC, EPI>;
+  // (a set-once note per device that the limit of dynamic LDS has been raised; racing first calls both
+  // set it, which is harmless)
+  static std::atomic<uint64_t> configured{0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return -1;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev >= 64 || !(configured.load(std::memory_order_acquire) & bit)) {
+    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return -1;
+    if (dev < 64) configured.fetch_or(bit, std::memory_order_release);
+  }
+  const int bnh = EPI == EPI_GLU ? BN / 2 : BN;
+  const int tiles_m = (a.M + BM - 1) / BM;
+  const int64_t tiles = (int64_t)tiles_m * ((a.n_store + bnh - 1) / bnh) * (a.twin ? 2 : 1);
+  if (tiles > 0x7fffffff) return -1;
+  PlainArgs g = a;
+  // as many row tiles per group as make an XCD's tiles read the fewest rows of both operands
+  const int per_cu = lds <= 80 * 1024 ? 2 : 1;
+  const int r = (int)std::max<int64_t>(1, std::min<int64_t>(32 * per_cu, tiles / 8));
+  g.group_m = std::max(1, std::min(tiles_m, (int)(sqrt((double)r * BN / BM) + 0.5)));
+  hipLaunchKernelGGL(kern, dim3((unsigned)tiles, a.n_split), dim3(WGM * WGN * 64), lds, st, g);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+// tile shapes: 0 128x128 (fp32 64x64 wavefront tiles as well), 1 256x256 (bf16)
+struct Plan { int shape, split; };
+constexpr int MAX_SPLIT_TILES = 512;   // a reduction is cut to fill one round of the machine, two workgroups a CU
+
+static Plan plain_plan(int64_t M, int64_t N, int64_t K, int planes, int segs, int bf16) {
+  const int64_t slabs = segs * ((K + (bf16 ? 31 : 15)) / (bf16 ? 32 : 16));
+  const int64_t big = ((M + 255) / 256) * ((N * planes + 255) / 256);
+  if (bf16 && big >= 224) return {1, 1};
+  const int64_t tiles = ((M + 127) / 128) * ((N * planes + 127) / 128);
+  int split = 1;
+  while (split < 16 && tiles * split * 2 <= MAX_SPLIT_TILES && slabs / (split * 2) >= 8) split *= 2;
+  return {0, split};
+}
+
+template <typename T, bool AMC, bool BMC, int EPI>
+static int launch_shape(const PlainArgs& a, int shape, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (shape == 1) return launch_tile<T, 256, 256, 2, 4, 4, AMC, BMC, EPI>(a, st);
+  }
+  return launch_tile<T, 128, 128, 2, 2, 4, AMC, BMC, EPI>(a, st);
+}
+
+template <typename T, int EPI>
+static int launch_reduce(const PlainArgs& a, hipStream_t st) {
+  const int64_t n = (int64_t)a.M * ((a.n_store + 7) / 8) * (a.twin ? 2 : 1);
+  hipLaunchKernelGGL((plain_reduce_kernel<T, EPI>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+template <typename T>
+static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) {
+  int rc = -1;
+  if (epi == EPI_OUT) {
+    if (!a.a_mc && a.b_mc) rc = launch_shape<T, false, true, EPI_OUT>(a, shape, st);
+    else if (!a.a_mc && !a.b_mc) rc = launch_shape<T, false, false, EPI_OUT>(a, shape, st);
+    else if (a.a_mc && a.b_mc) rc = launch_shape<T, true, true, EPI_OUT>(a, shape, st);
+    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_OUT>(a, st);
+  } else if (epi == EPI_GLU && !a.a_mc && a.b_mc) {
+    rc = launch_shape<T, false, true, EPI_GLU>(a, shape, st);
+    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GLU>(a, st);
+  } else if (epi == EPI_GELU && !a.a_mc && a.b_mc) {
+    rc = launch_shape<T, false, true, EPI_GELU>(a, shape, st);
+    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GELU>(a, st);
+  } else if (epi == EPI_GRAD && !a.a_mc && !a.b_mc) {
+    rc = launch_shape<T, false, false, EPI_GRAD>(a, shape, st);
+    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GRAD>(a, st);
+  }
+  return rc;
+}
+
+// (at most MAX_SPLIT_TILES tiles of 128 x 128 sums; the second plane's columns count as further columns)
+size_t plain_part_room() { return (size_t)MAX_SPLIT_TILES * 128 * 128 * 4; }
+
+int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st) {
+  if (a.M <= 0 || a.N <= 0) return 0;
+  if ((a.lda & 7) || (a.ldb & 7) || (a.segs != 1 && a.segs != 2) || a.n_store < a.N) return -1;
+  // a lane's offset inside a tile stays below 2 GiB
+  if (a.lda > (1 << 20) || a.ldb > (1 << 20)) return -1;
+  const int planes = epi == EPI_GLU || a.twin ? 2 : 1;
+  const Plan pl = plain_plan(a.M, a.N, a.K, planes, a.segs, bf16);
+  a.n_split = pl.split;
+  a.part = pl.split > 1 ? part : nullptr;
+  a.ldp = (a.N + 7) / 8 * 8;
+  return bf16 ? launch_typed<uint16_t>(a, epi, pl.shape, st) : launch_typed<float>(a, epi, pl.shape, st);
+}
+
+int launch_pad_rows(const void* src, void* dst, int64_t rows, int cols, int bf16, hipStream_t st) {
+  const int cols8 = (cols + 7) / 8 * 8;
+  const int64_t n = rows * cols8;
+  if (n <= 0) return 0;
+  const dim3 grid((unsigned)std::min<int64_t>((n + 1023) / 1024, 2048));
+  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)src, (uint16_t*)dst, rows, cols, cols8);
+  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, dim3(256), 0, st, (const uint32_t*)src, (uint32_t*)dst, rows, cols, cols8);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+}  // namespace ffsplit
