@@ -25,7 +25,8 @@
 namespace ffsplit {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-typedef __attribute__((address_space(3))) s16x4_t* lfrag_t;
+template <typename T>
+using lds_ptr = __attribute__((address_space(3))) T*;
 
 union Frag {
   u32x4_t u;
@@ -38,9 +39,14 @@ template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
 }
-__device__ __forceinline__ void wait_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+template <int N>
+__device__ __forceinline__ void wait_lgkmcnt() {
+  __builtin_amdgcn_s_waitcnt(0xc07f | ((N < 15 ? N : 15) << 8));
+}
 // workgroup barrier without a memory fence (the kernel orders its loads with explicit counters)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+#define FFS_ORDER __builtin_amdgcn_sched_barrier(0)   // instructions keep the written order
 
 __device__ __forceinline__ int xcd_remap(int i, int total) {
   const int q = total >> 3, rem = total & 7, x = i & 7;
@@ -133,24 +139,26 @@ struct Side {
     const uint32_t k = 4 * g;
     return k * P + (((j >> 2) ^ mc_swizzle(k)) * 16) + (j & 3) * 4;
   }
-  // fragment of the 16-row tile x of this side
-  static __device__ __forceinline__ void read(Frag& f, char* region, uint32_t lane, int x) {
+  // fragment of the 16-row tile x of this side; `region` (uniform): where it begins in LDS
+  static __device__ __forceinline__ void read(Frag& f, uint32_t region, uint32_t lane, int x) {
     if (!MC) {
-      f.u = *(const u32x4_t*)(region + x * 1024 + lane);
+      f.u = *(lds_ptr<const u32x4_t>)(uintptr_t)(region + x * 1024 + lane);
       return;
     }
     constexpr int TPS = SUB / 16;
     constexpr uint32_t TB = 16 * sizeof(T);     // bytes of a tile's piece of an LDS row
-    char* const at = region + (x / TPS) * (BK * P) + (lane ^ ((uint32_t)(x % TPS) * TB));
+    const uint32_t at = region + (x / TPS) * (BK * P) + (lane ^ ((uint32_t)(x % TPS) * TB));
     if (sizeof(T) == 2) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lfrag_t)(at + u * 4 * P)));
+        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)(at + u * 4 * P)));
     } else {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) f.f[t] = *(const float*)(at + t * P);
+      for (int t = 0; t < 4; ++t) f.f[t] = *(lds_ptr<const float>)(uintptr_t)(at + t * P);
     }
   }
+  // LDS reads of one fragment (16-byte ones are not merged; fp32 rows may be)
+  static constexpr int READS = MC ? (sizeof(T) == 2 ? 2 : 4) : 1;
 };
 
 template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, bool AMC, bool BMC, int EPI>
@@ -168,7 +176,7 @@ plain_kernel(const PlainArgs p) {
   constexpr int STAGE = (A_BLK + B_BLK) * 1024;
   static_assert(A_BLK % NW == 0 && B_BLK % NW == 0, "blocks divide over the wavefronts");
   static_assert(!PAIR || HB % NW == 0 || NW % HB == 0, "a load belongs to one matrix");
-  static_assert(STAGES >= 2 && STAGES <= 5 && STAGES * LPW <= 63, "loads in flight must fit the counter");
+  static_assert(STAGES >= 3 && STAGES <= 5 && STAGES * LPW <= 63, "loads in flight must fit the counter");
   static_assert(TM % 2 == 0 && (!PAIR || TN % 2 == 0), "row tiles are stored in pairs");
 
   extern __shared__ u32x4_t smem_v[];
@@ -203,23 +211,32 @@ plain_kernel(const PlainArgs p) {
   const int64_t a_org = (AMC ? (int64_t)m0 : (int64_t)m0 * p.lda) * (int)sizeof(T);
   const int64_t b_org = (BMC ? (int64_t)n0 : (int64_t)n0 * p.ldb) * (int)sizeof(T);
   const int64_t a_step = AMC ? (int64_t)BK * p.lda * (int)sizeof(T) : 64, b_step = BMC ? (int64_t)BK * p.ldb * (int)sizeof(T) : 64;
+  const uint32_t lds0 = lds_offset((const char*)smem);
 
-  // all loads of slab s0 + rel into a stage
-  auto issue = [&](int rel, int stage) {
-    int s = s0 + rel, seg = 0;
-    if (s >= ns) { s -= ns; seg = 1; }   // (segs = 2)
-    const int64_t ao = a_org + s * a_step, bo = b_org + s * b_step;
-    const char* const a0 = uniform((const char*)(seg ? p.A[1] : p.A[0]) + ao);
-    const char* const b0 = uniform((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo);
-    const char* const b1 = PAIR ? uniform((const char*)p.B[1] + bo) : b0;
-    const int al = bytes_left(p.a_bytes, ao), bl = bytes_left(p.b_bytes, bo);
-    const bool a_out = !AMC && s * BK + (int)ca * SA::EPC >= k_end, b_out = !BMC && s * BK + (int)cb * SA::EPC >= k_end;
-    const uint32_t st = lds_offset(smem) + stage * STAGE;
-#pragma unroll
-    for (int i = 0; i < LA; ++i) load_to_lds(a0, al, st + (wave + i * NW) * 1024, a_out ? NOWHERE : va[i]);
-#pragma unroll
-    for (int i = 0; i < LB; ++i)
-      load_to_lds(PAIR && (wave + i * NW) >= HB ? b1 : b0, bl, st + (A_BLK + wave + i * NW) * 1024, b_out ? NOWHERE : vb[i]);
+  // The slab whose loads go out next: its number within its segment and where it begins.
+  int next = s0 >= ns ? s0 - ns : s0, seg = s0 >= ns;   // (segs = 2)
+  int64_t ao = a_org + next * a_step, bo = b_org + next * b_step;
+  struct Source { const char *a, *b0, *b1; int al, bl; bool a_out, b_out; } src;
+  auto aim = [&]() {
+    src.a = uniform((const char*)(seg ? p.A[1] : p.A[0]) + ao);
+    src.b0 = uniform((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo);
+    src.b1 = PAIR ? uniform((const char*)p.B[1] + bo) : src.b0;
+    src.al = bytes_left(p.a_bytes, ao);
+    src.bl = bytes_left(p.b_bytes, bo);
+    src.a_out = !AMC && next * BK + (int)ca * SA::EPC >= k_end;
+    src.b_out = !BMC && next * BK + (int)cb * SA::EPC >= k_end;
+    ++next; ao += a_step; bo += b_step;
+    if (next == ns) { next = 0; seg = 1; ao = a_org; bo = b_org; }
+  };
+  // load number i of that slab into a stage
+  auto issue = [&](int i, int stage) {
+    const uint32_t st = lds0 + stage * STAGE;
+    if (i < LA) {
+      load_to_lds(src.a, src.al, st + (wave + i * NW) * 1024, src.a_out ? NOWHERE : va[i]);
+    } else {
+      const int b = wave + (i - LA) * NW;
+      load_to_lds(PAIR && b >= HB ? src.b1 : src.b0, src.bl, st + (A_BLK + b) * 1024, src.b_out ? NOWHERE : vb[i - LA]);
+    }
   };
 
   f32x4_t acc[TM][TN];
@@ -229,42 +246,97 @@ plain_kernel(const PlainArgs p) {
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   const uint32_t la = SA::lane_part(lane), lb = SB::lane_part(lane);
+  Frag fa[TM], fb[2][TN];
+  auto read_a = [&](int i, uint32_t st) { SA::read(fa[i], st, la, wm * TM + i); };
+  auto read_b = [&](int set, int j, uint32_t st) {
+    const int half = PAIR ? j / (TN / 2) : 0, jj = PAIR ? j % (TN / 2) : j;
+    SB::read(fb[set][j], st + (A_BLK + half * HB) * 1024, lb, wn * (PAIR ? TN / 2 : TN) + jj);
+  };
+  auto mma = [&](int set, int i, int j) {
+    if constexpr (sizeof(T) == 2) {
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][j].v, fa[i].v, acc[i][j], 0, 0, 0);
+    } else {
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-    if (s < nk) issue(s, s);
-  int stage = 0;
-  for (int s = 0; s < nk; ++s) {
-    const int later = min(STAGES - 2, nk - 1 - s);   // younger slabs that may still be in flight
+      for (int t = 0; t < 4; ++t)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[set][j].f[t], fa[i].f[t], acc[i][j], 0, 0, 0);
+    }
+  };
+  // at most `later` slabs of loads may still be in flight
+  auto wait_slabs = [&](int later) {
     if (later <= 0) wait_vmcnt<0>();
     else if (later == 1) wait_vmcnt<LPW>();
     else if (later == 2) wait_vmcnt<2 * LPW>();
     else wait_vmcnt<3 * LPW>();
-    wait_lgkmcnt0();
-    lds_barrier();   // slab s is there for all; all are done with slab s - 1
-    if (s + STAGES - 1 < nk) issue(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-    char* const st = smem + stage * STAGE;
-    Frag fa[TM], fb[TN];
+  };
+
+  // Step s multiplies slab s, whose fragments are in registers, and reads those of slab s + 1: the left
+  // operand's fragment i as soon as the MFMAs that use it are issued, the right operand's into a second
+  // set.  The barrier in the middle of the step, where the reads that it waits for were issued half a step
+  // before, retires slab s and publishes slab s + 2; the loads of slab s + STAGES go out behind it.
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int half = PAIR ? j / (TN / 2) : 0, jj = PAIR ? j % (TN / 2) : j;
-      // (the column tiles of a wavefront lie within one sub-block or are whole ones)
-      SB::read(fb[j], st + A_BLK * 1024 + half * HB * 1024, lb, wn * (PAIR ? TN / 2 : TN) + jj);
+  for (int s = 0; s < STAGES; ++s)
+    if (s < nk) {
+      aim();
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) issue(i, s);
     }
+  int stage = 0;   // stage of slab s
+  if (nk > 0) {
+    wait_slabs(min(nk, STAGES) - 2);   // slabs 0 and 1
+    lds_barrier();
 #pragma unroll
-    for (int i = 0; i < TM; ++i) SA::read(fa[i], st, la, wm * TM + i);
+    for (int j = 0; j < TN; ++j) read_b(0, j, lds0);
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) read_a(i, lds0);
+  }
+  auto step = [&](int s, auto setc, auto fullc) {
+    constexpr int set = decltype(setc)::value;
+    constexpr bool FULL = decltype(fullc)::value;   // every slab referred to exists
+    constexpr int RB = TM / 2 - 1;                  // the barrier follows this row
+    // reads of this step issued in front of the barrier
+    constexpr int YOUNGER = sizeof(T) == 2 ? (RB + 1) * SA::READS + ((RB + 1) * TN + TM - 1) / TM * SB::READS : 0;
+    const int ns1 = stage + 1 == STAGES ? 0 : stage + 1;
+    const uint32_t nx = lds0 + ns1 * STAGE;         // (past the end: stale data that is never used)
+    const int put = s + STAGES;
+    FFS_ORDER;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        if constexpr (sizeof(T) == 2) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j].v, fa[i].v, acc[i][j], 0, 0, 0);
-        } else {
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j].f[t], fa[i].f[t], acc[i][j], 0, 0, 0);
-        }
+      for (int jj = 0; jj < TN; ++jj) {
+        mma(set, i, (i & 1) ? TN - 1 - jj : jj);
+        FFS_ORDER;
+#pragma unroll
+        for (int q = 0; q < TN; ++q)
+          if (q * TM == i * TN + jj) read_b(set ^ 1, q, nx);
+        FFS_ORDER;
       }
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
+      read_a(i, nx);
+      FFS_ORDER;
+      if (i == RB) {
+        if (FULL) wait_vmcnt<(STAGES - 3) * LPW>();
+        else wait_slabs(min(nk - 1, put - 1) - (s + 2));
+        wait_lgkmcnt<YOUNGER>();
+        lds_barrier();
+        if (FULL || put < nk) aim();
+        FFS_ORDER;
+      }
+      if (i > RB) {
+#pragma unroll
+        for (int l = 0; l < LPW; ++l)
+          if (l * (TM - RB - 1) / LPW == i - RB - 1 && (FULL || put < nk)) issue(l, stage);
+        FFS_ORDER;
+      }
+    }
+    stage = ns1;
+  };
+  int s = 0;
+  for (; s + 1 + STAGES < nk; s += 2) {
+    step(s, std::integral_constant<int, 0>{}, std::true_type{});
+    step(s + 1, std::integral_constant<int, 1>{}, std::true_type{});
+  }
+  for (; s < nk; s += 2) {
+    step(s, std::integral_constant<int, 0>{}, std::false_type{});
+    if (s + 1 < nk) step(s + 1, std::integral_constant<int, 1>{}, std::false_type{});
   }
 
   // Store.  A lane holds columns 4 (l >> 4) .. + 3 of row l & 15 of each tile; exchanging lane rows
