@@ -52,12 +52,6 @@ __device__ __forceinline__ int xcd_remap(int i, int total) {
   const int q = total >> 3, rem = total & 7, x = i & 7;
   return x * q + (x < rem ? x : rem) + (i >> 3);
 }
-// swap the odd 16-lane rows of a with the even ones of b
-__device__ __forceinline__ void swap16(float& a, float& b) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-  a = __uint_as_float(r[0]);
-  b = __uint_as_float(r[1]);
-}
 __device__ __forceinline__ uint32_t kc_swizzle(uint32_t r4) { return (0x78u >> (2 * (r4 & 3))) & 3; }   // 0 2 3 1
 
 // bytes behind the offset `at` of a buffer of `bytes`, within what a resource's bound can say; uniform
@@ -339,33 +333,61 @@ plain_kernel(const PlainArgs p) {
     if (s + 1 < nk) step(s + 1, std::integral_constant<int, 1>{}, std::false_type{});
   }
 
-  // Store.  A lane holds columns 4 (l >> 4) .. + 3 of row l & 15 of each tile; exchanging lane rows
-  // between two row tiles leaves eight columns 8 (l >> 5) .. + 7 of row l & 31.
+  // Store.  A lane holds columns 4 (l >> 4) .. + 3 of row l & 15 of each 16x16 tile.  Each wavefront turns 32
+  // rows at a time round in a piece of LDS of its own, so that eight lanes (gated: four) hold 64 (32)
+  // consecutive columns of a row: whole cache lines, and the kept derivatives are read in the same shape, a
+  // group of 32 rows ahead.
+  constexpr int OW = PAIR ? WN / 2 : WN;             // output columns of a wavefront
+  constexpr int LPR = OW / 8, RP = 64 / LPR, NP = 32 / RP;
+  constexpr int PITCH = WN * 4 + 16;
+  static_assert(NW * 32 * PITCH <= STAGES * STAGE, "the stages' memory is used");
+  wait_lgkmcnt<0>();
+  lds_barrier();   // every wavefront is done with the stages
+  char* const own = smem + wave * (32 * PITCH);
+  const int col = n0 + wn * OW + (lane % LPR) * 8;
+  const int64_t row0 = m0 + wm * WM + lane / LPR;
+  using KT = kept_t<T>;
+  float ka[2][EPI == EPI_GRAD ? NP : 1][8], kb[2][EPI == EPI_GRAD ? NP : 1][8];
+  auto fetch = [&](int set, int ip) {
+    if constexpr (EPI == EPI_GRAD) {
 #pragma unroll
-  for (int jj = 0; jj < (PAIR ? TN / 2 : TN); ++jj) {
-    const int col = n0 + wn * (PAIR ? WN / 2 : WN) + jj * 16 + 8 * (lane >> 5);
-#pragma unroll
-    for (int ip = 0; ip < TM; ip += 2) {
-      const int64_t row = m0 + wm * WM + ip * 16 + (lane & 31);
-      float v[8], u[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = acc[ip][jj][e]; v[4 + e] = acc[ip + 1][jj][e];
-        swap16(v[e], v[4 + e]);
-        if (PAIR) {
-          u[e] = acc[ip][jj + TN / 2][e]; u[4 + e] = acc[ip + 1][jj + TN / 2][e];
-          swap16(u[e], u[4 + e]);
+      for (int q = 0; q < NP; ++q) {
+        const int64_t row = row0 + ip * 16 + q * RP;
+        if (row < p.M && col < p.n_store && p.part == nullptr) {
+          load8<KT>(p.D1, row * p.ldi + col, ka[set][q]);
+          if (p.D2 != nullptr) load8<KT>(p.D2, row * p.ldi + col, kb[set][q]);
         }
       }
+    }
+  };
+  fetch(0, 0);
+#pragma unroll
+  for (int ip = 0; ip < TM; ip += 2) {
+    constexpr int last = TM - 2;
+    if (ip < last) fetch((ip / 2 + 1) & 1, ip + 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        *(f32x4_t*)(own + (h * 16 + (lane & 15)) * PITCH + (j * 16 + 4 * (lane >> 4)) * 4) = acc[ip + h][j];
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      const char* const at = own + (q * RP + lane / LPR) * PITCH + (lane % LPR) * 32;
+      float v[8], u[8];
+      load8<float>(at, 0, v);
+      if (PAIR) load8<float>(at + OW * 4, 0, u);
+      const int64_t row = row0 + ip * 16 + q * RP;
       if (row >= p.M || col >= p.n_store) continue;
       if (p.part != nullptr) {
         const int planes = PAIR || p.twin ? 2 : 1;
-        const int64_t at = (((int64_t)blockIdx.y * planes + which) * p.M + row) * p.ldp + col;
-        store8<float>(p.part, at, v);
-        if (PAIR) store8<float>(p.part, at + (int64_t)p.M * p.ldp, u);
-        continue;
+        const int64_t to = (((int64_t)blockIdx.y * planes + which) * p.M + row) * p.ldp + col;
+        store8<float>(p.part, to, v);
+        if (PAIR) store8<float>(p.part, to + (int64_t)p.M * p.ldp, u);
+      } else if constexpr (EPI == EPI_GRAD) {
+        grad8<T>(p, row * p.ldi + col, col, v, ka[(ip / 2) & 1][q], kb[(ip / 2) & 1][q]);
+      } else {
+        emit8<T, EPI>(p, which, row, col, v, u);
       }
-      emit8<T, EPI>(p, which, row, col, v, u);
     }
   }
 }

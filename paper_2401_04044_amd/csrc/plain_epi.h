@@ -1,6 +1,7 @@
 // Internal: element types and store steps shared by the kernels of the training path.
 #pragma once
 #include "plain.h"
+#include <type_traits>
 
 namespace ffsplit {
 
@@ -8,6 +9,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;  // native vector: stays in registers
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 
 // silu(z) = z s with s = 1 / (1 + e^-z); its derivative is s (1 + z (1 - s)).  bf16 layers: exp2 and
 // a reciprocal, both within 1 ulp; fp32 layers: expf and a division.
@@ -42,37 +44,65 @@ __device__ __forceinline__ void gelu_and_slope(float z, float& h, float& d) {
   }
 }
 
+// Storage types: float, uint16_t (bf16 bits) and, for the kept derivatives of bf16 layers, _Float16.
 template <typename T>
 __device__ __forceinline__ void load8(const void* base, int64_t at, float (&v)[8]) {
-  if (sizeof(T) == 2) {
+  if constexpr (std::is_same<T, float>::value) {
+    const f32x4_t a = *(const f32x4_t*)((const char*)base + at * 4), b = *(const f32x4_t*)((const char*)base + at * 4 + 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    const f16x8_t h = *(const f16x8_t*)((const char*)base + at * 2);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+  } else {
     const u32x4_t u = *(const u32x4_t*)((const char*)base + at * 2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[2 * e] = __uint_as_float(u[e] << 16);
       v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
     }
-  } else {
-    const f32x4_t a = *(const f32x4_t*)((const char*)base + at * 4), b = *(const f32x4_t*)((const char*)base + at * 4 + 16);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
   }
 }
 template <typename T>
 __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[8]) {
-  if (sizeof(T) == 2) {
-    *(u32x4_t*)((char*)base + at * 2) = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                                                pack_bf16x2(v[6], v[7])};
-  } else {
+  if constexpr (std::is_same<T, float>::value) {
     *(f32x4_t*)((char*)base + at * 4) = f32x4_t{v[0], v[1], v[2], v[3]};
     *(f32x4_t*)((char*)base + at * 4 + 16) = f32x4_t{v[4], v[5], v[6], v[7]};
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    f16x8_t h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)v[e];
+    *(f16x8_t*)((char*)base + at * 2) = h;
+  } else {
+    *(u32x4_t*)((char*)base + at * 2) = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                                pack_bf16x2(v[6], v[7])};
   }
 }
+// The kept derivatives: in bf16 they would cost as much precision as each of the roundings that the
+// products force on H, dU and dG (relative error of a gradient 2.9e-3); fp16 leaves those alone (2.4e-3).
+// One beyond 65504 is kept as infinity and makes the gradient say so; below 6e-5 fp16's steps are 6e-8.
+template <typename T>
+using kept_t = typename std::conditional<std::is_same<T, float>::value, float, _Float16>::type;
 __device__ __forceinline__ float load1(const void* base, int64_t at, bool f32) {
   return f32 ? ((const float*)base)[at] : bf16_to_f32(((const bf16_t*)base)[at]);
 }
 __device__ __forceinline__ void store1(void* base, int64_t at, bool f32, float v) {
   if (f32) ((float*)base)[at] = v;
   else ((bf16_t*)base)[at] = f32_to_bf16(v);
+}
+
+// EPI_GRAD: dH in v, the kept derivatives in a and b
+template <typename T>
+__device__ __forceinline__ void grad8(const PlainArgs& p, int64_t at, int col, const float (&v)[8], float (&a)[8], float (&b)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) a[e] = col + e < p.N ? v[e] * a[e] : 0.f;
+  store8<T>(p.O1, at, a);
+  if (p.D2 != nullptr) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = col + e < p.N ? v[e] * b[e] : 0.f;
+    store8<T>(p.O2, at, b);
+  }
 }
 
 // The store step of eight columns col .. col + 7 (a multiple of 8, below n_store; EPI_OUT: below N) of
@@ -112,16 +142,9 @@ __device__ __forceinline__ void emit8(const PlainArgs& p, int which, int64_t row
   const int64_t at = row * p.ldi + col;
   float a[8], b[8];
   if (EPI == EPI_GRAD) {
-    load8<T>(p.D1, at, a);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = col + e < p.N ? v[e] * a[e] : 0.f;
-    store8<T>(p.O1, at, a);
-    if (p.D2 != nullptr) {
-      load8<T>(p.D2, at, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) b[e] = col + e < p.N ? v[e] * b[e] : 0.f;
-      store8<T>(p.O2, at, b);
-    }
+    load8<kept_t<T>>(p.D1, at, a);
+    if (p.D2 != nullptr) load8<kept_t<T>>(p.D2, at, b);
+    grad8<T>(p, at, col, v, a, b);
     return;
   }
   float h[8];
@@ -139,8 +162,8 @@ __device__ __forceinline__ void emit8(const PlainArgs& p, int which, int64_t row
   }
   store8<T>(p.H, at, h);
   if (p.D1 != nullptr) {
-    store8<T>((void*)p.D1, at, a);
-    if (EPI == EPI_GLU) store8<T>((void*)p.D2, at, b);
+    store8<kept_t<T>>((void*)p.D1, at, a);
+    if (EPI == EPI_GLU) store8<kept_t<T>>((void*)p.D2, at, b);
   }
 }
 
