@@ -54,31 +54,30 @@ __device__ __forceinline__ int xcd_remap(int i, int total) {
 }
 __device__ __forceinline__ uint32_t kc_swizzle(uint32_t r4) { return (0x78u >> (2 * (r4 & 3))) & 3; }   // 0 2 3 1
 
-// bytes behind the offset `at` of a buffer of `bytes`, within what a resource's bound can say; uniform
-__device__ __forceinline__ int bytes_left(int64_t bytes, int64_t at) {
-  const int64_t left = bytes - at;
-  const int hi = __builtin_amdgcn_readfirstlane((int)(left >> 31)), lo = __builtin_amdgcn_readfirstlane((int)left);
-  return hi > 0 ? 0x7fffffff : hi < 0 ? 0 : lo;
-}
-// (the resource is built in scalar registers; the builtin returns a signed int)
-__device__ __forceinline__ const char* uniform(const char* q) {
-  const uint64_t u = (uint64_t)q;
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
-  return (const char*)(((uint64_t)hi << 32) | (uint64_t)lo);
-}
-constexpr uint32_t NOWHERE = 0x80000000u;   // beyond every bound
-// 16 bytes per lane from base + offset (zeros beyond `bytes`) straight into LDS, lane l to dst + 16 l.
-// base, bytes and dst in scalar registers.  In assembly because the compiler, when it sees a load into
-// LDS, waits for all of them before every turned-round LDS read; here the counts are kept by hand.  (The
-// first s_nop covers scalar registers just written by v_readfirstlane, the second m0.)
-__device__ __forceinline__ void load_to_lds(const char* base, int bytes, uint32_t dst, uint32_t offset) {
-  const uint64_t b = (uint64_t)base;
-  const u32x4_t r = {(uint32_t)b, (uint32_t)(b >> 32), (uint32_t)bytes, 0x00027000u};
-  asm volatile("s_nop 4\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+constexpr uint32_t NOWHERE = 0x80000000u;   // beyond every resource's end
+constexpr uint32_t FAR = 1u << 30;          // a resource is set anew before a scalar offset passes this
+// 16 bytes per lane from the buffer r at offset + soff (zeros beyond its end) straight into LDS, lane l to
+// dst + 16 l; r, dst and soff in scalar registers.  In assembly because the compiler, when it sees a load
+// into LDS, waits for all of them before every turned-round LDS read; here the counts are kept by hand.
+// (The s_nop covers m0, which nothing else in these kernels uses.)
+__device__ __forceinline__ void load_to_lds(const u32x4_t& r, uint32_t dst, uint32_t offset, uint32_t soff) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen lds"
                :
-               : "v"(offset), "s"(r), "s"(dst)
-               : "memory");   // (m0: nothing else in these kernels uses it)
+               : "v"(offset), "s"(r), "s"(dst), "s"(soff)
+               : "memory");
+}
+// A buffer resource for what lies from base on, `left` bytes, in scalar registers.  (The s_nop keeps the
+// distance that a load needs from the v_readfirstlane that wrote them.)
+__device__ __forceinline__ u32x4_t resource(const char* base, int64_t left) {
+  const uint64_t b = (uint64_t)base;
+  u32x4_t r;
+  r[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+  r[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
+  const int hi = __builtin_amdgcn_readfirstlane((int)(left >> 31)), lo = __builtin_amdgcn_readfirstlane((int)left);
+  r[2] = hi > 0 ? 0x7fffffffu : hi < 0 ? 0u : (uint32_t)lo;
+  r[3] = 0x00027000u;
+  asm volatile("s_nop 4" : "+s"(r));
+  return r;
 }
 __device__ __forceinline__ uint32_t lds_offset(const char* q) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)q;
@@ -108,7 +107,7 @@ struct Side {
     if (P == 256) return 4 * ((k >> 2) & 3);
     return 4 * ((k >> 2) & 1);
   }
-  // byte offset of the lane's 16 bytes of block b from the tile's first element, and (kc) its chunk
+  // byte offset of the lane's 16 bytes of block b from the tile's first element; kc: chunk, its number in the slab
   static __device__ __forceinline__ uint32_t source(int b, int lane, uint32_t ld, uint32_t* chunk) {
     if (!MC) {
       const uint32_t r = lane >> 2, c = (lane & 3) ^ kc_swizzle(r >> 2);
@@ -118,7 +117,6 @@ struct Side {
     constexpr int CPR = P / 16;   // chunks of an LDS row
     const uint32_t sub = b / BPS, k = (b % BPS) * KPB + lane / CPR;
     const uint32_t c = (lane % CPR) ^ mc_swizzle(k);
-    *chunk = 0;
     return k * ld * (uint32_t)sizeof(T) + sub * P + c * 16;
   }
   // the lane's part of a fragment address: rows l & 15 of a 16-row tile, elements 8 (l >> 4) .. + 7
@@ -133,22 +131,28 @@ struct Side {
     const uint32_t k = 4 * g;
     return k * P + (((j >> 2) ^ mc_swizzle(k)) * 16) + (j & 3) * 4;
   }
-  // fragment of the 16-row tile x of this side; `region` (uniform): where it begins in LDS
-  static __device__ __forceinline__ void read(Frag& f, uint32_t region, uint32_t lane, int x) {
+  // where a wavefront's fragments begin, from the side's beginning in a stage: its first tile is x0, a
+  // multiple of the number of tiles it has (which divides TPS, or is a multiple of it)
+  static constexpr int TPS = SUB / 16;
+  static constexpr uint32_t TB = 16 * sizeof(T);     // mc: bytes of a tile's piece of an LDS row
+  static __device__ __forceinline__ uint32_t first(int x0, int lane) {
+    if (!MC) return x0 * 1024 + lane_part(lane);
+    return (x0 / TPS) * (BK * P) + (lane_part(lane) ^ ((uint32_t)(x0 % TPS) * TB));
+  }
+  // fragment of the tile x0 + i; at: that beginning in LDS
+  static __device__ __forceinline__ void read(Frag& f, uint32_t at, int i) {
     if (!MC) {
-      f.u = *(lds_ptr<const u32x4_t>)(uintptr_t)(region + x * 1024 + lane);
+      f.u = *(lds_ptr<const u32x4_t>)(uintptr_t)(at + i * 1024);
       return;
     }
-    constexpr int TPS = SUB / 16;
-    constexpr uint32_t TB = 16 * sizeof(T);     // bytes of a tile's piece of an LDS row
-    const uint32_t at = region + (x / TPS) * (BK * P) + (lane ^ ((uint32_t)(x % TPS) * TB));
+    const uint32_t a = (at ^ ((uint32_t)(i % TPS) * TB)) + (i / TPS) * (BK * P);
     if (sizeof(T) == 2) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)(at + u * 4 * P)));
+        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)(a + u * 4 * P)));
     } else {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) f.f[t] = *(lds_ptr<const float>)(uintptr_t)(at + t * P);
+      for (int t = 0; t < 4; ++t) f.f[t] = *(lds_ptr<const float>)(uintptr_t)(a + t * P);
     }
   }
   // LDS reads of one fragment (16-byte ones are not merged; fp32 rows may be)
@@ -197,41 +201,57 @@ plain_kernel(const PlainArgs p) {
   const int nk = max(0, min(total, s0 + per) - s0);
   const int k_end = (p.K + SA::EPC - 1) / SA::EPC * SA::EPC;   // kc: chunks from here on read as zero
 
-  uint32_t va[LA], vb[LB], ca = 0, cb = 0;
+  uint32_t va[LA], vb[LB], chunk = 0;
 #pragma unroll
-  for (int i = 0; i < LA; ++i) va[i] = SA::source(wave + i * NW, lane, (uint32_t)p.lda, &ca);
+  for (int i = 0; i < LA; ++i) va[i] = SA::source(wave + i * NW, lane, (uint32_t)p.lda, &chunk);
 #pragma unroll
-  for (int i = 0; i < LB; ++i) vb[i] = SB::source((wave + i * NW) % HB, lane, (uint32_t)p.ldb, &cb);
+  for (int i = 0; i < LB; ++i) vb[i] = SB::source((wave + i * NW) % HB, lane, (uint32_t)p.ldb, &chunk);
   const int64_t a_org = (AMC ? (int64_t)m0 : (int64_t)m0 * p.lda) * (int)sizeof(T);
   const int64_t b_org = (BMC ? (int64_t)n0 : (int64_t)n0 * p.ldb) * (int)sizeof(T);
-  const int64_t a_step = AMC ? (int64_t)BK * p.lda * (int)sizeof(T) : 64, b_step = BMC ? (int64_t)BK * p.ldb * (int)sizeof(T) : 64;
+  const uint32_t a_step = AMC ? BK * (uint32_t)p.lda * (uint32_t)sizeof(T) : 64, b_step = BMC ? BK * (uint32_t)p.ldb * (uint32_t)sizeof(T) : 64;
   const uint32_t lds0 = lds_offset((const char*)smem);
+  const uint32_t st0 = lds0 + wave * 1024;
+  // kc: the chunks behind the reduction's end, in the last slab of a segment
+  const uint32_t beyond = (!AMC || !BMC) && (ns - 1) * BK + (int)chunk * SA::EPC >= k_end ? NOWHERE : 0u;
 
-  // The slab whose loads go out next: its number within its segment and where it begins.
-  int next = s0 >= ns ? s0 - ns : s0, seg = s0 >= ns;   // (segs = 2)
-  int64_t ao = a_org + next * a_step, bo = b_org + next * b_step;
-  struct Source { const char *a, *b0, *b1; int al, bl; bool a_out, b_out; } src;
+  // The slab whose loads go out next: its number within its segment, and scalar offsets from where the
+  // resources begin.  Behind the last slab the resources are empty: the loads then put zeros into stages
+  // (which a reduction of an odd number of slabs multiplies once), and every step issues and awaits the same
+  // number of loads.
+  int next = s0, seg = 0;
+  if (s0 >= ns) { next -= ns; seg = 1; }   // (segs = 2)
+  int todo = nk, event = 0;                // slabs still to be loaded, and until the resources change
+  const int reach = __builtin_amdgcn_readfirstlane((int)(FAR / max(a_step, b_step)));
+  u32x4_t ra, rb0, rb1;
+  uint32_t sa = 0, sb = 0;
   auto aim = [&]() {
-    src.a = uniform((const char*)(seg ? p.A[1] : p.A[0]) + ao);
-    src.b0 = uniform((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo);
-    src.b1 = PAIR ? uniform((const char*)p.B[1] + bo) : src.b0;
-    src.al = bytes_left(p.a_bytes, ao);
-    src.bl = bytes_left(p.b_bytes, bo);
-    src.a_out = !AMC && next * BK + (int)ca * SA::EPC >= k_end;
-    src.b_out = !BMC && next * BK + (int)cb * SA::EPC >= k_end;
-    ++next; ao += a_step; bo += b_step;
-    if (next == ns) { next = 0; seg = 1; ao = a_org; bo = b_org; }
+    if (next == ns) { next = 0; seg = 1; }
+    const int64_t ao = a_org + next * (int64_t)a_step, bo = b_org + next * (int64_t)b_step;
+    ra = resource((const char*)(seg ? p.A[1] : p.A[0]) + ao, todo > 0 ? p.a_bytes - ao : 0);
+    rb0 = resource((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo, todo > 0 ? p.b_bytes - bo : 0);
+    if (PAIR) rb1 = resource((const char*)p.B[1] + bo, todo > 0 ? p.b_bytes - bo : 0);
+    sa = 0; sb = 0;
+    // (a resource's end and a lane's offset are 32-bit: it is left behind before the scalar offset passes FAR)
+    event = todo > 0 ? min(min(todo, ns - next), reach) : 0x7fffffff;
   };
   // load number i of that slab into a stage
   auto issue = [&](int i, int stage) {
-    const uint32_t st = lds0 + stage * STAGE;
+    const uint32_t st = st0 + stage * STAGE;
+    const uint32_t out = next == ns - 1 ? beyond : 0u;
     if (i < LA) {
-      load_to_lds(src.a, src.al, st + (wave + i * NW) * 1024, src.a_out ? NOWHERE : va[i]);
+      load_to_lds(ra, st + i * NW * 1024, AMC ? va[i] : va[i] | out, sa);
     } else {
-      const int b = wave + (i - LA) * NW;
-      load_to_lds(PAIR && b >= HB ? src.b1 : src.b0, src.bl, st + (A_BLK + b) * 1024, src.b_out ? NOWHERE : vb[i - LA]);
+      const int b = i - LA;
+      // (gated: load b NW + wave belongs to the second matrix from HB on)
+      const bool second = PAIR && (HB >= NW ? b * NW >= HB : (wave + b * NW) >= HB);
+      load_to_lds(second ? rb1 : rb0, st + (A_BLK + b * NW) * 1024, BMC ? vb[b] : vb[b] | out, sb);
     }
   };
+  auto advance = [&]() {
+    ++next; --todo; sa += a_step; sb += b_step;
+    if (--event == 0) aim();
+  };
+  aim();
 
   f32x4_t acc[TM][TN];
 #pragma unroll
@@ -239,13 +259,11 @@ plain_kernel(const PlainArgs p) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  const uint32_t la = SA::lane_part(lane), lb = SB::lane_part(lane);
+  constexpr int TNH = PAIR ? TN / 2 : TN;   // column tiles of one matrix
+  const uint32_t la = lds0 + SA::first(wm * TM, lane), lb = lds0 + A_BLK * 1024 + SB::first(wn * TNH, lane);
   Frag fa[TM], fb[2][TN];
-  auto read_a = [&](int i, uint32_t st) { SA::read(fa[i], st, la, wm * TM + i); };
-  auto read_b = [&](int set, int j, uint32_t st) {
-    const int half = PAIR ? j / (TN / 2) : 0, jj = PAIR ? j % (TN / 2) : j;
-    SB::read(fb[set][j], st + (A_BLK + half * HB) * 1024, lb, wn * (PAIR ? TN / 2 : TN) + jj);
-  };
+  auto read_a = [&](int i, uint32_t st) { SA::read(fa[i], la + st, i); };
+  auto read_b = [&](int set, int j, uint32_t st) { SB::read(fb[set][j], lb + st + (j / TNH) * HB * 1024, j % TNH); };
   auto mma = [&](int set, int i, int j) {
     if constexpr (sizeof(T) == 2) {
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][j].v, fa[i].v, acc[i][j], 0, 0, 0);
@@ -255,43 +273,30 @@ plain_kernel(const PlainArgs p) {
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[set][j].f[t], fa[i].f[t], acc[i][j], 0, 0, 0);
     }
   };
-  // at most `later` slabs of loads may still be in flight
-  auto wait_slabs = [&](int later) {
-    if (later <= 0) wait_vmcnt<0>();
-    else if (later == 1) wait_vmcnt<LPW>();
-    else if (later == 2) wait_vmcnt<2 * LPW>();
-    else wait_vmcnt<3 * LPW>();
-  };
-
   // Step s multiplies slab s, whose fragments are in registers, and reads those of slab s + 1: the left
   // operand's fragment i as soon as the MFMAs that use it are issued, the right operand's into a second
   // set.  The barrier in the middle of the step, where the reads that it waits for were issued half a step
   // before, retires slab s and publishes slab s + 2; the loads of slab s + STAGES go out behind it.
 #pragma unroll
-  for (int s = 0; s < STAGES; ++s)
-    if (s < nk) {
-      aim();
+  for (int s = 0; s < STAGES; ++s) {
 #pragma unroll
-      for (int i = 0; i < LPW; ++i) issue(i, s);
-    }
-  int stage = 0;   // stage of slab s
-  if (nk > 0) {
-    wait_slabs(min(nk, STAGES) - 2);   // slabs 0 and 1
-    lds_barrier();
-#pragma unroll
-    for (int j = 0; j < TN; ++j) read_b(0, j, lds0);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) read_a(i, lds0);
+    for (int i = 0; i < LPW; ++i) issue(i, s);
+    advance();
   }
-  auto step = [&](int s, auto setc, auto fullc) {
+  wait_vmcnt<(STAGES - 2) * LPW>();   // slabs 0 and 1
+  lds_barrier();
+#pragma unroll
+  for (int j = 0; j < TN; ++j) read_b(0, j, 0);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) read_a(i, 0);
+  int stage = 0;   // stage of slab s
+  auto step = [&](auto setc) {
     constexpr int set = decltype(setc)::value;
-    constexpr bool FULL = decltype(fullc)::value;   // every slab referred to exists
     constexpr int RB = TM / 2 - 1;                  // the barrier follows this row
     // reads of this step issued in front of the barrier
     constexpr int YOUNGER = sizeof(T) == 2 ? (RB + 1) * SA::READS + ((RB + 1) * TN + TM - 1) / TM * SB::READS : 0;
     const int ns1 = stage + 1 == STAGES ? 0 : stage + 1;
-    const uint32_t nx = lds0 + ns1 * STAGE;         // (past the end: stale data that is never used)
-    const int put = s + STAGES;
+    const uint32_t nx = ns1 * STAGE;
     FFS_ORDER;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -307,31 +312,26 @@ plain_kernel(const PlainArgs p) {
       read_a(i, nx);
       FFS_ORDER;
       if (i == RB) {
-        if (FULL) wait_vmcnt<(STAGES - 3) * LPW>();
-        else wait_slabs(min(nk - 1, put - 1) - (s + 2));
+        wait_vmcnt<(STAGES - 3) * LPW>();
         wait_lgkmcnt<YOUNGER>();
         lds_barrier();
-        if (FULL || put < nk) aim();
         FFS_ORDER;
       }
       if (i > RB) {
 #pragma unroll
         for (int l = 0; l < LPW; ++l)
-          if (l * (TM - RB - 1) / LPW == i - RB - 1 && (FULL || put < nk)) issue(l, stage);
+          if (l * (TM - RB - 1) / LPW == i - RB - 1) issue(l, stage);
         FFS_ORDER;
       }
     }
+    advance();
     stage = ns1;
   };
-  int s = 0;
-  for (; s + 1 + STAGES < nk; s += 2) {
-    step(s, std::integral_constant<int, 0>{}, std::true_type{});
-    step(s + 1, std::integral_constant<int, 1>{}, std::true_type{});
+  for (int s = 0; s < nk; s += 2) {
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
   }
-  for (; s < nk; s += 2) {
-    step(s, std::integral_constant<int, 0>{}, std::false_type{});
-    if (s + 1 < nk) step(s + 1, std::integral_constant<int, 1>{}, std::false_type{});
-  }
+  wait_vmcnt<0>();
 
   // Store.  A lane holds columns 4 (l >> 4) .. + 3 of row l & 15 of each 16x16 tile.  Each wavefront turns 32
   // rows at a time round in a piece of LDS of its own, so that eight lanes (gated: four) hold 64 (32)
@@ -347,15 +347,15 @@ plain_kernel(const PlainArgs p) {
   const int col = n0 + wn * OW + (lane % LPR) * 8;
   const int64_t row0 = m0 + wm * WM + lane / LPR;
   using KT = kept_t<T>;
-  float ka[2][EPI == EPI_GRAD ? NP : 1][8], kb[2][EPI == EPI_GRAD ? NP : 1][8];
+  Raw8<KT> ka[2][EPI == EPI_GRAD ? NP : 1], kb[2][EPI == EPI_GRAD ? NP : 1];
   auto fetch = [&](int set, int ip) {
     if constexpr (EPI == EPI_GRAD) {
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
         const int64_t row = row0 + ip * 16 + q * RP;
         if (row < p.M && col < p.n_store && p.part == nullptr) {
-          load8<KT>(p.D1, row * p.ldi + col, ka[set][q]);
-          if (p.D2 != nullptr) load8<KT>(p.D2, row * p.ldi + col, kb[set][q]);
+          ka[set][q].load(p.D1, row * p.ldi + col);
+          if (p.D2 != nullptr) kb[set][q].load(p.D2, row * p.ldi + col);
         }
       }
     }
@@ -384,7 +384,10 @@ plain_kernel(const PlainArgs p) {
         store8<float>(p.part, to, v);
         if (PAIR) store8<float>(p.part, to + (int64_t)p.M * p.ldp, u);
       } else if constexpr (EPI == EPI_GRAD) {
-        grad8<T>(p, row * p.ldi + col, col, v, ka[(ip / 2) & 1][q], kb[(ip / 2) & 1][q]);
+        float a[8], b[8];
+        ka[(ip / 2) & 1][q].get(a);
+        kb[(ip / 2) & 1][q].get(b);
+        grad8<T>(p, row * p.ldi + col, col, v, a, b);
       } else {
         emit8<T, EPI>(p, which, row, col, v, u);
       }

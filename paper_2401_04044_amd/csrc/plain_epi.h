@@ -64,6 +64,16 @@ __device__ __forceinline__ void load8(const void* base, int64_t at, float (&v)[8
     }
   }
 }
+// eight of them as loaded
+template <typename T>
+struct Raw8 {
+  u32x4_t u[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const void* base, int64_t at) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = *(const u32x4_t*)((const char*)base + at * (int)sizeof(T) + 16 * i);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const { load8<T>(u, 0, v); }
+};
 template <typename T>
 __device__ __forceinline__ void store8(void* base, int64_t at, const float (&v)[8]) {
   if constexpr (std::is_same<T, float>::value) {
