@@ -1,4 +1,5 @@
 """ctypes binding: same names as the C ABI, argument marshalling only."""
+import contextlib
 import ctypes
 import os
 
@@ -297,22 +298,36 @@ def stack_forward(desc, splits, x, b1_packed=None, b2=None, eps=1e-6, workspace=
 _DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
 
-def _take(t, what, shape, dtypes, device):
+def _take(t, what, shape, dtype, device):
     """A tensor argument of the training calls: they take plain row-major matrices, so that a view with
     strides, another type or another device is an error here and not a wrong result there."""
     if t is None:
         return None
-    if not isinstance(dtypes, tuple):
-        dtypes = (dtypes,)
-    if t.dtype not in dtypes:
-        raise TypeError(f"{what}: {t.dtype}, wanted {' or '.join(map(str, dtypes))}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype and t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, wanted {dtype}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(t.shape)}, wanted {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: not contiguous")
     if t.device != device:
         raise ValueError(f"{what}: on {t.device}, wanted {device}")
     return t
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _raw_stream(device):
+    """The current stream of a device, without the stream object that _stream() makes (5 us of a 10 us call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+
+def _on(device):
+    """The device of the tensors made current, for the stream, the scratch and the launches."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors on {device}, wanted a GPU")
+    return _HERE_ALREADY if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
 def _take_layer(desc, W1, Wg, W2, device, what=""):
@@ -358,10 +373,10 @@ def dense_forward(desc, X, W1, Wg, W2, Y=None, residual=None, y_f32=False, want_
         if saved is None:
             saved = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         _take_kept(saved, need, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         ws = _scratch(workspace_bytes(desc, WS_DENSE_FORWARD, T), workspace, dev)
         rc = lib.ffsplit_dense_forward(ctypes.byref(desc), _ptr(X), T, _ptr(W1), _ptr(Wg), _ptr(W2), _ptr(Y), _ptr(residual),
-                                       1 if y_f32 else 0, _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _stream())
+                                       1 if y_f32 else 0, _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _raw_stream(dev))
     _check(rc, "ffsplit_dense_forward")
     return (Y, saved) if keep else Y
 
@@ -404,11 +419,11 @@ def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=
         dX = torch.empty((T, desc.d_model), dtype=dt, device=dev)
     _take(dX, "dX", (T, desc.d_model), dt, dev)
     g = _grads_for(desc, grads, accumulate, grad_f32, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         ws = _scratch(workspace_bytes(desc, WS_DENSE_BACKWARD, T), workspace, dev)
         rc = lib.ffsplit_dense_backward(ctypes.byref(desc), _ptr(X), T, _ptr(W1), _ptr(Wg), _ptr(W2), _ptr(saved), _ptr(dY),
                                         _ptr(dX), _ptr(g["W1"]), _ptr(g["Wg"]), _ptr(g["W2"]),
-                                        _grad_flags(accumulate, grad_f32), _ptr(ws), ws.numel(), _stream())
+                                        _grad_flags(accumulate, grad_f32), _ptr(ws), ws.numel(), _raw_stream(dev))
     _check(rc, "ffsplit_dense_backward")
     return dX, g
 
@@ -416,68 +431,97 @@ def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=
 def token_rmsnorm_backward(x, dn, eps=1e-6, residual=None, dx=None, want_cast=False):
     """Gradient of x behind token_rmsnorm: dx = [residual +] r dn - x r^3 mean(x dn), fp32 [T, d] (residual may
     be dx).  Returns dx, or (dx, dx in dn's type) with want_cast."""
-    T, d = x.shape
-    dev = x.device
-    _take(x, "x", (T, d), torch.float32, dev)
-    _take(dn, "dn", (T, d), (torch.float32, torch.bfloat16), dev)
-    _take(residual, "residual", (T, d), torch.float32, dev)
+    shape, dev = x.shape, x.device
+    T, d = shape
+    _take(x, "x", None, torch.float32, dev)
+    bf16 = dn.dtype == torch.bfloat16
+    _take(dn, "dn", shape, torch.bfloat16 if bf16 else torch.float32, dev)
+    _take(residual, "residual", shape, torch.float32, dev)
     if dx is None:
         dx = torch.empty_like(x)
-    _take(dx, "dx", (T, d), torch.float32, dev)
+    else:
+        _take(dx, "dx", shape, torch.float32, dev)
     cast = torch.empty_like(dn) if want_cast else None
-    with torch.cuda.device(dev):
-        rc = lib.ffsplit_token_rmsnorm_backward(_ptr(x), _ptr(dn), T, d, ctypes.c_float(eps),
-                                                BF16 if dn.dtype == torch.bfloat16 else F32, _ptr(residual), _ptr(dx),
-                                                _ptr(cast), _stream())
+    with _on(dev):
+        rc = lib.ffsplit_token_rmsnorm_backward(x.data_ptr(), dn.data_ptr(), T, d, eps, BF16 if bf16 else F32, _ptr(residual),
+                                                dx.data_ptr(), _ptr(cast), _raw_stream(dev))
     _check(rc, "ffsplit_token_rmsnorm_backward")
     return (dx, cast) if want_cast else dx
 
 
-def _grad_list(grads, what="gradients"):
-    n = len(grads)
-    dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
-    counts, dtypes = (ctypes.c_int64 * max(n, 1))(), (ctypes.c_int32 * max(n, 1))()
-    for i, g in enumerate(grads):
-        _take(g, what, None, (torch.float32, torch.bfloat16), dev)
-        counts[i] = g.numel()
-        dtypes[i] = F32 if g.dtype == torch.float32 else BF16
-    return n, dev, counts, dtypes
+class _GradList:
+    """The host arrays that describe a list of gradients."""
+
+    def __init__(self, grads):
+        n = self.n = len(grads)
+        self.device = dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        ptrs, counts, dtypes = [], [], []
+        for g in grads:
+            dt = g.dtype
+            if dt != torch.float32 and dt != torch.bfloat16:
+                raise TypeError(f"gradients: {dt}, wanted torch.float32 or torch.bfloat16")
+            if not g.is_contiguous() or g.device != dev:
+                raise ValueError(f"gradients: contiguous tensors on one device are wanted ({dev})")
+            ptrs.append(g.data_ptr())
+            counts.append(g.numel())
+            dtypes.append(F32 if dt == torch.float32 else BF16)
+        self.ptrs, self.counts = (ctypes.c_void_p * max(n, 1))(*ptrs), (ctypes.c_int64 * max(n, 1))(*counts)
+        self.dtypes = (ctypes.c_int32 * max(n, 1))(*dtypes)
+
+    def out_ptrs(self, grads, out):
+        if out is None:
+            return self.ptrs
+        if len(out) != self.n:
+            raise ValueError(f"out: {len(out)} tensors for {self.n} gradients")
+        ptrs = []
+        for g, o in zip(grads, out):
+            if o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous() or o.device != self.device:
+                raise ValueError("out: tensors like the gradients are wanted, contiguous and on their device")
+            ptrs.append(o.data_ptr())
+        return (ctypes.c_void_p * max(self.n, 1))(*ptrs)
+
+    def norm(self, norm, flag, workspace):
+        dev = self.device
+        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else _take(norm, "norm", (1,), torch.float32, dev)
+        flag = torch.empty(1, dtype=torch.int32, device=dev) if flag is None else _take(flag, "flag", (1,), torch.int32, dev)
+        ws = _scratch(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, self.n), workspace, dev)
+        _check(lib.ffsplit_grad_norm(self.n, self.ptrs, self.counts, self.dtypes, norm.data_ptr(), flag.data_ptr(), ws.data_ptr(),
+                                     ws.numel(), _raw_stream(dev)), "ffsplit_grad_norm")
+        return norm, flag
+
+    def clip(self, norm, max_norm, out_ptrs):
+        dev = self.device
+        _check(lib.ffsplit_grad_clip(self.n, self.ptrs, self.counts, self.dtypes, norm.data_ptr(), max_norm, out_ptrs,
+                                     _raw_stream(dev)), "ffsplit_grad_clip")
 
 
 def grad_norm(grads, norm=None, flag=None, workspace=None):
     """Norm over all elements of all tensors.  Returns (norm [1] fp32, flag [1] int32), on the device; the flag is
     E_NONFINITE if the norm is not finite, else 0."""
-    n, dev, counts, dtypes = _grad_list(grads)
-    with torch.cuda.device(dev):
-        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else _take(norm, "norm", (1,), torch.float32, dev)
-        flag = torch.empty(1, dtype=torch.int32, device=dev) if flag is None else _take(flag, "flag", (1,), torch.int32, dev)
-        ws = _scratch(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, n), workspace, dev)
-        rc = lib.ffsplit_grad_norm(n, _ptrs(grads), counts, dtypes, _ptr(norm), _ptr(flag), _ptr(ws), ws.numel(), _stream())
-    _check(rc, "ffsplit_grad_norm")
-    return norm, flag
+    g = _GradList(grads)
+    with _on(g.device):
+        return g.norm(norm, flag, workspace)
 
 
 def grad_clip(grads, norm, max_norm, out=None):
     """out = grads * min(1, max_norm / norm), in place without `out`; unchanged where the norm (on the device) is
     not finite.  Returns the list of clipped gradients."""
-    n, dev, counts, dtypes = _grad_list(grads)
-    out = grads if out is None else out
-    if len(out) != n:
-        raise ValueError(f"out: {len(out)} tensors for {n} gradients")
-    for g, o in zip(grads, out):
-        _take(o, "out", g.shape, g.dtype, dev)
-    _take(norm, "norm", (1,), torch.float32, dev)
-    with torch.cuda.device(dev):
-        rc = lib.ffsplit_grad_clip(n, _ptrs(grads), counts, dtypes, _ptr(norm), ctypes.c_float(max_norm), _ptrs(out),
-                                   _stream())
-    _check(rc, "ffsplit_grad_clip")
-    return out
+    g = _GradList(grads)
+    to = g.out_ptrs(grads, out)
+    _take(norm, "norm", (1,), torch.float32, g.device)
+    with _on(g.device):
+        g.clip(norm, max_norm, to)
+    return grads if out is None else out
 
 
 def clip_grad_norm(grads, max_norm, out=None, workspace=None):
     """grad_norm, then grad_clip.  Returns (norm, flag, clipped gradients)."""
-    norm, flag = grad_norm(grads, workspace=workspace)
-    return norm, flag, grad_clip(grads, norm, max_norm, out)
+    g = _GradList(grads)
+    to = g.out_ptrs(grads, out)
+    with _on(g.device):
+        norm, flag = g.norm(None, None, workspace)
+        g.clip(norm, max_norm, to)
+    return norm, flag, grads if out is None else out
 
 
 def _stack_args(desc, layers, device):
@@ -500,10 +544,10 @@ def dense_stack_forward(desc, layers, x, eps=1e-6, want_saved=False, saved=None,
             saved = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         _take_kept(saved, need, dev)
     W1, Wg, W2 = _stack_args(desc, layers, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         ws = _scratch(workspace_bytes(desc, WS_DENSE_STACK, T), workspace, dev)
         rc = lib.ffsplit_dense_stack_forward(ctypes.byref(desc), n, W1, Wg, W2, _ptr(x), T, ctypes.c_float(eps),
-                                             _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _stream())
+                                             _ptr(saved) if keep else None, _ptr(ws), ws.numel(), _raw_stream(dev))
     _check(rc, "ffsplit_dense_stack_forward")
     return saved if keep else x
 
@@ -521,7 +565,7 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
          for l in range(n)]
     W1, Wg, W2 = _stack_args(desc, layers, dev)
     gated = desc.act == ACT_SWIGLU
-    with torch.cuda.device(dev):
+    with _on(dev):
         norm = torch.empty(1, dtype=torch.float32, device=dev)
         flag = torch.empty(1, dtype=torch.int32, device=dev)
         need = max(workspace_bytes(desc, WS_DENSE_STACK, T), int(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, 3 * n)))
@@ -530,7 +574,7 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
                                               ctypes.c_float(eps), _ptrs([q["W1"] for q in g]),
                                               _ptrs([q["Wg"] for q in g]) if gated else None, _ptrs([q["W2"] for q in g]),
                                               _grad_flags(accumulate, grad_f32), ctypes.c_float(max_norm), _ptr(norm),
-                                              _ptr(flag), _ptr(ws), ws.numel(), _stream())
+                                              _ptr(flag), _ptr(ws), ws.numel(), _raw_stream(dev))
     _check(rc, "ffsplit_dense_stack_backward")
     return g, norm, flag
 

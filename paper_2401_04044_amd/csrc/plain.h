@@ -10,7 +10,7 @@ namespace ffsplit {
 //   EPI_GLU   H = silu(Z) U, and if D1 is set D1 = dH/dU = silu(Z), D2 = dH/dZ = U silu'(Z)
 //   EPI_GELU  H = gelu(S), and if D1 is set D1 = gelu'(S)
 //   EPI_GRAD  O1 = S * D1 and, with D2, O2 = S * D2
-// H, D1, D2, O1, O2 have rows of ldi elements and n_store >= N stored columns; those from N on are
+// H, D1, D2, O1, O2 have rows of ldi elements and n_store (N rounded up to 8) stored columns; those from N on are
 // stored as zeros, so that a later reduction over them in whole 16-byte chunks adds nothing.
 enum { EPI_OUT = 0, EPI_GLU = 1, EPI_GELU = 2, EPI_GRAD = 3 };
 
@@ -52,7 +52,7 @@ struct PlainArgs {
 size_t plain_part_room();
 // part: that many bytes
 int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st);
-// dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind; cols8 = cols rounded up to 8
-int launch_pad_rows(const void* src, void* dst, int64_t rows, int cols, int bf16, hipStream_t st);
+// dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind, of one or two matrices; cols8 = cols rounded up to 8
+int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int64_t rows, int cols, int bf16, hipStream_t st);
 
 }  // namespace ffsplit

@@ -174,7 +174,7 @@ plain_kernel(const PlainArgs p) {
   constexpr int STAGE = (A_BLK + B_BLK) * 1024;
   static_assert(A_BLK % NW == 0 && B_BLK % NW == 0, "blocks divide over the wavefronts");
   static_assert(!PAIR || HB % NW == 0 || NW % HB == 0, "a load belongs to one matrix");
-  static_assert(STAGES >= 3 && STAGES <= 5 && STAGES * LPW <= 63, "loads in flight must fit the counter");
+  static_assert(STAGES >= 3 && STAGES * LPW <= 63, "loads in flight must fit the counter");
   static_assert(TM % 2 == 0 && (!PAIR || TN % 2 == 0), "row tiles are stored in pairs");
 
   extern __shared__ u32x4_t smem_v[];
@@ -396,37 +396,48 @@ plain_kernel(const PlainArgs p) {
 }
 
 // Sum of the ranges' fp32 sums in range order, and the store step.  One thread per row, plane of a twin
-// product and eight columns.
+// product and eight columns; four ranges are read at a time.
 template <typename T, int EPI>
-__global__ void __launch_bounds__(256) plain_reduce_kernel(const PlainArgs p) {
-  const int cpr = (p.n_store + 7) / 8;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
+  constexpr bool PAIR = EPI == EPI_GLU;
+  const int cpr = p.n_store / 8;
+  const int64_t id = (int64_t)blockIdx.x * 64 + threadIdx.x;
   const int64_t per_plane = (int64_t)p.M * cpr;
   const int which = p.twin && id >= per_plane;
   const int64_t in = which ? id - per_plane : id;
   if (in >= per_plane) return;
   const int64_t row = in / cpr;
   const int col = (int)(in % cpr) * 8;
-  const int planes = EPI == EPI_GLU || p.twin ? 2 : 1;
+  const int planes = PAIR || p.twin ? 2 : 1;
   const int64_t plane = (int64_t)p.M * p.ldp;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int s = 0; s < p.n_split; ++s) {
-    const int64_t at = ((int64_t)s * planes + which) * plane + row * p.ldp + col;
-    float w[8];
-    load8<float>(p.part, at, w);
+  for (int s0 = 0; s0 < p.n_split; s0 += 4) {
+    float w[4][8], x[PAIR ? 4 : 1][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
-    if (EPI == EPI_GLU) {
-      load8<float>(p.part, at + plane, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] += w[e];
+    for (int i = 0; i < 4; ++i) {
+      const int s = min(s0 + i, p.n_split - 1);
+      const int64_t at = ((int64_t)s * planes + which) * plane + row * p.ldp + col;
+      load8<float>(p.part, at, w[i]);
+      if (PAIR) load8<float>(p.part, at + plane, x[i]);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (s0 + i < p.n_split)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] += w[i][e];
+          if (PAIR) u[e] += x[i][e];
+        }
   }
   emit8<T, EPI>(p, which, row, col, v, u);
 }
 
+// blockIdx.y: which of the two matrices
 template <typename T>
-__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src, T* dst, int64_t rows, int cols, int cols8) {
+__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* src1, T* dst0, T* dst1, int64_t rows, int cols,
+                                                       int cols8) {
+  const T* const src = blockIdx.y ? src1 : src0;
+  T* const dst = blockIdx.y ? dst1 : dst0;
   const int64_t n = rows * cols8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / cols8;
@@ -463,32 +474,80 @@ static int launch_tile(const PlainArgs& a, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-// tile shapes: 0 128x128 (fp32 64x64 wavefront tiles as well), 1 256x256 (bf16)
+enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_128x256 = 3, PS_SHAPES = 4 };
 struct Plan { int shape, split; };
-constexpr int MAX_SPLIT_TILES = 512;   // a reduction is cut to fill one round of the machine, two workgroups a CU
 
-static Plan plain_plan(int64_t M, int64_t N, int64_t K, int planes, int segs, int bf16) {
-  const int64_t slabs = segs * ((K + (bf16 ? 31 : 15)) / (bf16 ? 32 : 16));
-  const int64_t big = ((M + 255) / 256) * ((N * planes + 255) / 256);
-  if (bf16 && big >= 224) return {1, 1};
-  const int64_t tiles = ((M + 127) / 128) * ((N * planes + 127) / 128);
-  int split = 1;
-  while (split < 16 && tiles * split * 2 <= MAX_SPLIT_TILES && slabs / (split * 2) >= 8) split *= 2;
-  return {0, split};
+// Choice of the tile and of the ranges that the reduction is cut into, by estimated time (us): t[k - 1] a slab with k
+// workgroups on a CU, per_cu of which a CU holds at a time, `fixed` for filling the ring and storing.  256 CUs; the
+// fullest one sets the time.  The figures are a least-squares fit to 3400 timings of 258 products (1 to 4096 rows, the
+// layers' widths from 256 to 5120) on every tile and up to 16 ranges; the chosen one takes 2 % (bf16) and 0.2 % (fp32)
+// longer than the best on average.
+struct ShapeCost { int bm, bn, per_cu; float t[4], fixed; };
+static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.246f, 0.452f}, 4.9f},
+                                                {256, 256, 1, {0.514f}, 7.0f},
+                                                {64, 64, 4, {0.138f, 0.227f, 0.497f, 0.546f}, 3.9f},
+                                                {128, 256, 2, {0.500f, 0.704f}, 5.6f}};
+static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {1.05f, 1.61f}, 1.6f}, {}, {64, 64, 4, {0.348f, 0.570f, 0.989f, 1.21f}, 0.3f}, {}};
+struct ProductCost {
+  float layout[3];        // factor of a slab: right operand mc, both kc, both mc
+  float bw, overlap;      // bytes a us, and the share of the traffic's time that comes on top
+  float sum, sum_range, sum_bw;   // adding ranges: a launch, each range, bytes a us
+};
+static const ProductCost COST_BF16 = {{1.0f, 1.08f, 1.17f}, 4.55e6f, 0.2f, 1.0f, 0.3f, 2.65e6f};
+static const ProductCost COST_F32 = {{1.0f, 0.98f, 1.06f}, 2.04e6f, 0.22f, 1.6f, 0.26f, 1.91e6f};
+constexpr size_t PART_ROOM = (size_t)32 << 20;   // scratch for ranges' sums
+
+static Plan plain_plan(const PlainArgs& a, int epi, int bf16) {
+  const ProductCost& c = bf16 ? COST_BF16 : COST_F32;
+  const int esz = bf16 ? 2 : 4, planes = epi == EPI_GLU || a.twin ? 2 : 1;
+  const int bk = bf16 ? 32 : 16, slabs = a.segs * ((a.K + bk - 1) / bk);
+  const float layout = c.layout[a.a_mc ? 2 : a.b_mc ? 0 : 1];
+  const int stored = epi == EPI_GLU ? 3 : epi == EPI_GELU ? 2 : epi == EPI_GRAD ? (a.D2 ? 4 : 2) : planes;
+  const float bytes = (float)esz * ((float)a.M * a.K * a.segs + (float)a.N * a.K * (planes > a.segs ? planes : a.segs) +
+                                    (float)stored * a.M * a.N);
+  Plan best = {PS_128x128, 1};
+  float best_t = 1e30f;
+  for (int s = 0; s < PS_SHAPES; ++s) {
+    const ShapeCost& q = bf16 ? SHAPE_BF16[s] : SHAPE_F32[s];
+    if (q.bm == 0) continue;
+    const int bn = epi == EPI_GLU && !(bf16 && s == PS_64x64) ? q.bn / 2 : q.bn;
+    const int64_t tiles = (int64_t)((a.M + q.bm - 1) / q.bm) * ((a.n_store + bn - 1) / bn) * (a.twin ? 2 : 1);
+    for (int split = 1; split <= 16; split += split < 4 ? 1 : split < 8 ? 2 : 4) {
+      const size_t part = (size_t)split * planes * a.M * a.n_store * 4;
+      if (split > 1 && (part > PART_ROOM || tiles * split > 768 || slabs / split < 4)) break;
+      const int n = (slabs + split - 1) / split;
+      const int64_t load = (tiles * split + 255) / 256, full = load / q.per_cu, rest = load % q.per_cu;
+      float t = (float)full * (n * q.t[q.per_cu - 1] * layout + q.fixed);
+      if (rest) t += n * q.t[rest - 1] * layout + q.fixed;
+      t += c.overlap * bytes / c.bw;
+      if (t < bytes / c.bw) t = bytes / c.bw;
+      if (split > 1) t += c.sum + c.sum_range * split + (float)part / c.sum_bw;
+      if (t < best_t) { best_t = t; best.shape = s; best.split = split; }
+    }
+  }
+  return best;
 }
 
 template <typename T, bool AMC, bool BMC, int EPI>
 static int launch_shape(const PlainArgs& a, int shape, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if (shape == 1) return launch_tile<T, 256, 256, 2, 4, 4, AMC, BMC, EPI>(a, st);
+  constexpr bool BF = sizeof(T) == 2;
+  switch (shape) {
+    case PS_128x128: return launch_tile<T, 128, 128, 2, 2, 5, AMC, BMC, EPI>(a, st);
+    case PS_64x64:   // (bf16 gated: 64 x 64 of each matrix)
+      return BF && EPI == EPI_GLU ? launch_tile<T, 64, 128, 2, 2, 6, AMC, BMC, EPI>(a, st)
+                                  : launch_tile<T, 64, BF && EPI == EPI_GLU ? 128 : 64, 2, 2, 8, AMC, BMC, EPI>(a, st);
   }
-  return launch_tile<T, 128, 128, 2, 2, 4, AMC, BMC, EPI>(a, st);
+  if constexpr (BF) {
+    if (shape == PS_256x256) return launch_tile<T, 256, 256, 2, 4, 4, AMC, BMC, EPI>(a, st);
+    if (shape == PS_128x256) return launch_tile<T, 128, 256, 1, 4, 3, AMC, BMC, EPI>(a, st);
+  }
+  return -1;
 }
 
 template <typename T, int EPI>
 static int launch_reduce(const PlainArgs& a, hipStream_t st) {
-  const int64_t n = (int64_t)a.M * ((a.n_store + 7) / 8) * (a.twin ? 2 : 1);
-  hipLaunchKernelGGL((plain_reduce_kernel<T, EPI>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+  const int64_t n = (int64_t)a.M * (a.n_store / 8) * (a.twin ? 2 : 1);
+  hipLaunchKernelGGL((plain_reduce_kernel<T, EPI>), dim3((unsigned)((n + 63) / 64)), dim3(64), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
@@ -513,29 +572,29 @@ static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) 
   return rc;
 }
 
-// (at most MAX_SPLIT_TILES tiles of 128 x 128 sums; the second plane's columns count as further columns)
-size_t plain_part_room() { return (size_t)MAX_SPLIT_TILES * 128 * 128 * 4; }
+size_t plain_part_room() { return PART_ROOM; }
 
 int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st) {
   if (a.M <= 0 || a.N <= 0) return 0;
   if ((a.lda & 7) || (a.ldb & 7) || (a.segs != 1 && a.segs != 2) || a.n_store < a.N) return -1;
   // a lane's offset inside a tile stays below 2 GiB
   if (a.lda > (1 << 20) || a.ldb > (1 << 20)) return -1;
-  const int planes = epi == EPI_GLU || a.twin ? 2 : 1;
-  const Plan pl = plain_plan(a.M, a.N, a.K, planes, a.segs, bf16);
+  const Plan pl = plain_plan(a, epi, bf16);
   a.n_split = pl.split;
   a.part = pl.split > 1 ? part : nullptr;
-  a.ldp = (a.N + 7) / 8 * 8;
+  a.ldp = a.n_store;
   return bf16 ? launch_typed<uint16_t>(a, epi, pl.shape, st) : launch_typed<float>(a, epi, pl.shape, st);
 }
 
-int launch_pad_rows(const void* src, void* dst, int64_t rows, int cols, int bf16, hipStream_t st) {
+int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int64_t rows, int cols, int bf16, hipStream_t st) {
   const int cols8 = (cols + 7) / 8 * 8;
   const int64_t n = rows * cols8;
   if (n <= 0) return 0;
-  const dim3 grid((unsigned)std::min<int64_t>((n + 1023) / 1024, 2048));
-  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)src, (uint16_t*)dst, rows, cols, cols8);
-  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, dim3(256), 0, st, (const uint32_t*)src, (uint32_t*)dst, rows, cols, cols8);
+  const dim3 grid((unsigned)std::min<int64_t>((n + 1023) / 1024, 2048), src1 ? 2 : 1);
+  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)src0, (const uint16_t*)src1,
+                               (uint16_t*)dst0, (uint16_t*)dst1, rows, cols, cols8);
+  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, dim3(256), 0, st, (const uint32_t*)src0, (const uint32_t*)src1,
+                          (uint32_t*)dst0, (uint32_t*)dst1, rows, cols, cols8);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

@@ -65,13 +65,9 @@ size_t kept_bytes(const Dense& s) { return (1 + s.planes) * s.act_bytes; }
 int aligned_weights(const Dense& s, const void* W1, const void* Wg, char* ws, const void** u, const void** g, hipStream_t st) {
   *u = W1; *g = Wg;
   if (!s.pad_bytes) return 0;
-  if (launch_pad_rows(W1, ws, s.d, s.f, s.bf16, st)) return -1;
   *u = ws;
-  if (s.gated) {
-    if (launch_pad_rows(Wg, ws + s.pad_bytes, s.d, s.f, s.bf16, st)) return -1;
-    *g = ws + s.pad_bytes;
-  }
-  return 0;
+  if (s.gated) *g = ws + s.pad_bytes;
+  return launch_pad_rows(W1, s.gated ? Wg : nullptr, ws, ws + s.pad_bytes, s.d, s.f, s.bf16, st);
 }
 
 PlainArgs product(int64_t M, int N, int64_t K) {
