@@ -261,22 +261,27 @@ plain_kernel(const PlainArgs p) {
 
   constexpr int TNH = PAIR ? TN / 2 : TN;   // column tiles of one matrix
   const uint32_t la = lds0 + SA::first(wm * TM, lane), lb = lds0 + A_BLK * 1024 + SB::first(wn * TNH, lane);
-  Frag fa[TM], fb[2][TN];
-  auto read_a = [&](int i, uint32_t st) { SA::read(fa[i], la + st, i); };
+  // DBL: the left operand's fragments in two sets as well
+  constexpr bool DBL = TM * TN <= 16;
+  Frag fa[DBL ? 2 : 1][TM], fb[2][TN];
+  auto read_a = [&](int set, int i, uint32_t st) { SA::read(fa[DBL ? set : 0][i], la + st, i); };
   auto read_b = [&](int set, int j, uint32_t st) { SB::read(fb[set][j], lb + st + (j / TNH) * HB * 1024, j % TNH); };
   auto mma = [&](int set, int i, int j) {
     if constexpr (sizeof(T) == 2) {
-      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][j].v, fa[i].v, acc[i][j], 0, 0, 0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][j].v, fa[DBL ? set : 0][i].v, acc[i][j], 0, 0, 0);
     } else {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[set][j].f[t], fa[i].f[t], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[set][j].f[t], fa[DBL ? set : 0][i].f[t], acc[i][j], 0, 0, 0);
     }
   };
-  // Step s multiplies slab s, whose fragments are in registers, and reads those of slab s + 1: the left
-  // operand's fragment i as soon as the MFMAs that use it are issued, the right operand's into a second
-  // set.  The barrier in the middle of the step, where the reads that it waits for were issued half a step
-  // before, retires slab s and publishes slab s + 2; the loads of slab s + STAGES go out behind it.
+  // Step s multiplies slab s, whose fragments are in registers, reads those of slab s + 1 and has one
+  // barrier, placed where the reads that it waits for were issued long before.
+  //   DBL (small wavefront tiles): the reads are dealt out over the first five eighths of the MFMAs; the
+  //     barrier after three quarters retires slab s + 1, which is in registers then, and publishes slab s + 2;
+  //     the loads of slab s + 1 + STAGES go out behind it.
+  //   otherwise: the left operand's fragment i is overwritten as soon as the MFMAs that use it are issued; the
+  //     barrier in the middle retires slab s and publishes slab s + 2; the loads of slab s + STAGES follow.
 #pragma unroll
   for (int s = 0; s < STAGES; ++s) {
 #pragma unroll
@@ -288,40 +293,74 @@ plain_kernel(const PlainArgs p) {
 #pragma unroll
   for (int j = 0; j < TN; ++j) read_b(0, j, 0);
 #pragma unroll
-  for (int i = 0; i < TM; ++i) read_a(i, 0);
+  for (int i = 0; i < TM; ++i) read_a(0, i, 0);
+  if (DBL) {
+    wait_lgkmcnt<0>();
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) issue(i, 0);
+    advance();
+  }
   int stage = 0;   // stage of slab s
   auto step = [&](auto setc) {
     constexpr int set = decltype(setc)::value;
-    constexpr int RB = TM / 2 - 1;                  // the barrier follows this row
-    // reads of this step issued in front of the barrier
-    constexpr int YOUNGER = sizeof(T) == 2 ? (RB + 1) * SA::READS + ((RB + 1) * TN + TM - 1) / TM * SB::READS : 0;
     const int ns1 = stage + 1 == STAGES ? 0 : stage + 1;
     const uint32_t nx = ns1 * STAGE;
     FFS_ORDER;
+    if constexpr (DBL) {
+      constexpr int NM = TM * TN, NR = TM + TN, RD = NM * 5 / 8, SYNC = NM * 3 / 4;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-#pragma unroll
-      for (int jj = 0; jj < TN; ++jj) {
-        mma(set, i, (i & 1) ? TN - 1 - jj : jj);
+      for (int q = 0; q < NM; ++q) {
+        const int i = q / TN, j = (i & 1) ? TN - 1 - q % TN : q % TN;
+        mma(set, i, j);
         FFS_ORDER;
 #pragma unroll
-        for (int q = 0; q < TN; ++q)
-          if (q * TM == i * TN + jj) read_b(set ^ 1, q, nx);
+        for (int r = 0; r < NR; ++r)
+          if (r * RD / NR == q) {
+            if (r < TN) read_b(set ^ 1, r, nx);
+            else read_a(set ^ 1, r - TN, nx);
+          }
         FFS_ORDER;
-      }
-      read_a(i, nx);
-      FFS_ORDER;
-      if (i == RB) {
-        wait_vmcnt<(STAGES - 3) * LPW>();
-        wait_lgkmcnt<YOUNGER>();
-        lds_barrier();
-        FFS_ORDER;
-      }
-      if (i > RB) {
+        if (q == SYNC - 1) {
+          wait_vmcnt<(STAGES - 2) * LPW>();
+          wait_lgkmcnt<0>();
+          lds_barrier();
+          FFS_ORDER;
+        }
 #pragma unroll
         for (int l = 0; l < LPW; ++l)
-          if (l * (TM - RB - 1) / LPW == i - RB - 1) issue(l, stage);
+          if (SYNC + l * (NM - SYNC) / LPW == q) issue(l, ns1);
         FFS_ORDER;
+      }
+    } else {
+      constexpr int RB = TM / 2 - 1;                  // the barrier follows this row
+      // reads of this step issued in front of the barrier
+      constexpr int YOUNGER = sizeof(T) == 2 ? (RB + 1) * SA::READS + ((RB + 1) * TN + TM - 1) / TM * SB::READS : 0;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int jj = 0; jj < TN; ++jj) {
+          mma(set, i, (i & 1) ? TN - 1 - jj : jj);
+          FFS_ORDER;
+#pragma unroll
+          for (int q = 0; q < TN; ++q)
+            if (q * TM == i * TN + jj) read_b(set ^ 1, q, nx);
+          FFS_ORDER;
+        }
+        read_a(0, i, nx);
+        FFS_ORDER;
+        if (i == RB) {
+          wait_vmcnt<(STAGES - 3) * LPW>();
+          wait_lgkmcnt<YOUNGER>();
+          lds_barrier();
+          FFS_ORDER;
+        }
+        if (i > RB) {
+#pragma unroll
+          for (int l = 0; l < LPW; ++l)
+            if (l * (TM - RB - 1) / LPW == i - RB - 1) issue(l, stage);
+          FFS_ORDER;
+        }
       }
     }
     advance();
