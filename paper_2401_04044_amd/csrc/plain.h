@@ -10,20 +10,32 @@ namespace ffsplit {
 //   EPI_GLU   H = silu(Z) U, and if D1 is set D1 = dH/dU = silu(Z), D2 = dH/dZ = U silu'(Z)
 //   EPI_GELU  H = gelu(S), and if D1 is set D1 = gelu'(S)
 //   EPI_GRAD  O1 = S * D1 and, with D2, O2 = S * D2
-// H, D1, D2, O1, O2 have rows of ldi elements and n_store (N rounded up to 8) stored columns; those from N on are
-// stored as zeros, so that a later reduction over them in whole 16-byte chunks adds nothing.
+// H, D1, D2, O1, O2 are [M, ldi] matrices (bf16: rows rounded up to 16; H, O1 and O2 in blocks, D1 and D2 row-major) with
+// n_store (N rounded up to 8) stored columns; those from N on are stored as zeros, so that a later reduction over
+// them in whole 16-byte chunks adds nothing.
 enum { EPI_OUT = 0, EPI_GLU = 1, EPI_GELU = 2, EPI_GRAD = 3 };
 
-// D[m, n] = sum_k A(m, k) B(n, k), fp32 accumulation.  An operand is stored with its reduction
-// contiguous ("kc": element (r, k) at r * ld + k) or its rows ("mc": at k * ld + r).  ld a multiple of
-// 8, pointers 16-byte aligned; kc: the elements from K to the next multiple of 8 are zero in at least
-// one operand and finite in the other.
+// How an operand's element (r, k) lies (see plain.hip): row-major with the reduction contiguous, r * ld + k, fetched a
+// slab (KC) or two (KC2) at a time; row-major with the rows contiguous, k * ld + r (MC); in blocks of 16 x 32
+// with r the token (BK) or k (BM).
+enum { LAY_KC = 0, LAY_KC2 = 1, LAY_MC = 2, LAY_BK = 3, LAY_BM = 4 };
+
+// bf16 activations of this path: element (t, j) of a [T, ldi] matrix.  Blocks of 16 tokens x 32 neurons, 1 KiB each,
+// [token block][neuron block]; in a block the 16-byte chunk c of token r lies at 4 r + (c ^ f(r / 4)), f = 0 2 3 1.
+// ldi a multiple of 32; T rounded up to 16, the rows behind the last token hold zeros.
+inline __host__ __device__ int64_t blocked_at(int64_t t, int j, int64_t ldi) {
+  const int r = (int)(t & 15), c = (j >> 3) & 3;
+  return ((t >> 4) * (ldi >> 5) + (j >> 5)) * 512 + (4 * r + (c ^ ((0x78 >> (2 * (r >> 2))) & 3))) * 8 + (j & 7);
+}
+
+// D[m, n] = sum_k A(m, k) B(n, k), fp32 accumulation.  ld a multiple of 8 (blocks: 32), pointers 16-byte aligned; KC,
+// KC2, BK: the elements from K to the next multiple of 8 are zero in at least one operand and finite in the other.
 struct PlainArgs {
   const void* A[2];
   const void* B[2];
   int64_t lda, ldb;
   int64_t a_bytes, b_bytes;   // of each: nothing at or beyond is read
-  int a_mc, b_mc;
+  int a_lay, b_lay;
   int M, N, K;
   // How the second operands take part:
   //   segs = 2   the reduction goes over A[0] B[0] and then A[1] B[1], K elements each

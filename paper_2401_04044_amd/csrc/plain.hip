@@ -6,14 +6,21 @@
 // A layer's forward and backward pass read the same matrices along different axes (X W1, dY W2^T,
 // X^T dU, ...), and its weights change every step: a copy re-tiled for each use would cost 10 to 20 %
 // of the products' time.  So one kernel takes each operand as it lies in memory:
-//   kc: reduction contiguous.  A slab of 64 bytes per row; the 16-byte chunk c of row r sits in LDS at
-//       4 r + (c ^ f(r / 4)), f = 0 2 3 1: the four lane groups that a 16-byte LDS read serves at a time
-//       (lanes 0-3, 12-15, 20-27 and so on) then fall into different banks.
-//   mc: rows contiguous.  bf16 fragments are turned round on the way out of LDS (ds_read_b64_tr_b16:
-//       lane j of 16 gets column j of four 16-column rows), fp32 ones are read element by element.
-//       The LDS rows' pieces are exchanged by an XOR with the row number, so that the eight rows read
-//       at a time fall into different banks.
-// Both go from global memory straight into a ring of LDS stages (buffer loads with LDS destination).
+//   KC   row-major, reduction contiguous, 64 bytes of a row per slab.  The 16-byte chunk c of row r sits in LDS at
+//        4 r + (c ^ f(r / 4)), f = 0 2 3 1: the lane groups that a 16-byte LDS read serves at a time (lanes
+//        0-3, 12-15, 20-27 and so on) then fall into different banks.
+//   KC2  the same fetched two slabs at a time, 128 bytes of a row: half the requests.  (64 bytes a row cost the
+//        memory pipeline up to a third of its rate: 4096 x 4096 x 22016 with both operands KC 614 us, with
+//        contiguous ones 460.)  A pair of slabs needs a third more LDS than its half of a ring of single ones, so
+//        that only one operand of a product can be fetched this way.
+//   MC   row-major, rows contiguous.  bf16 fragments are turned round on the way out of LDS (ds_read_b64_tr_b16:
+//        lane j of 16 gets column j of four 16-column rows), fp32 ones are read element by element.  Pieces of the
+//        LDS rows are exchanged by an XOR with the row number, so that the eight rows read at a time fall into
+//        different banks.  As fast as contiguous loads.
+//   BK, BM  this path's own activations in bf16 (H, dU, dG), stored in blocks of 16 tokens x 32 neurons (1 KiB)
+//        whose chunks lie as KC has them in LDS: every load is a contiguous 1 KiB, whether the reduction goes
+//        over the neurons (BK) or over the tokens (BM, turned round like MC).
+// All go from global memory straight into rings of LDS stages (buffer loads with LDS destination).
 // The buffers' bounds are exact: what lies behind an operand's end reads as zero, which is how a
 // reduction that ends inside a slab and rows behind the last are handled, without masks in the loop.
 #include "plain_epi.h"
@@ -83,21 +90,24 @@ __device__ __forceinline__ uint32_t lds_offset(const char* q) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)q;
 }
 
-// One operand's side of the tile: R rows, in LDS at byte `region` of a stage.
-// Blocks of 1 KiB, one load instruction each: kc 16 rows x 64 bytes; mc 1024 / P k-rows x P bytes, P the
-// length of an LDS row (256 bytes, or the whole side if that is shorter).
-template <typename T, int R, bool MC>
+// One operand's side of the tile: R rows of one matrix.  Blocks of 1 KiB, one load instruction each: KC 16
+// rows x 64 bytes; KC2 8 rows x 128 bytes; MC 1024 / P k-rows x P bytes, P the length of an LDS row (256 bytes, or the
+// whole side if that is shorter); BK, BM a stored block.
+template <typename T, int R, int LAY>
 struct Side {
   static constexpr int EPC = 16 / sizeof(T);          // elements per 16-byte chunk
   static constexpr int BK = 4 * EPC;                  // depth of a slab
+  static constexpr bool TURNED = LAY == LAY_MC || LAY == LAY_BM;
+  static constexpr int UNIT = LAY == LAY_KC2 ? 2 : 1; // slabs fetched together
+  static constexpr int UNIT_BYTES = UNIT * R * 64;
   static constexpr int P = R * (int)sizeof(T) < 256 ? R * (int)sizeof(T) : 256;
-  static constexpr int SUB = P / (int)sizeof(T);      // mc: rows of the operand in one sub-block
-  static constexpr int KPB = 1024 / P;                // mc: k-rows of one load
-  static constexpr int BPS = BK / KPB;                // mc: loads of one sub-block
-  static constexpr int BLOCKS = R / 16;
-  static_assert(P == 256 || P == 128, "the exchange of pieces is written for these");
+  static constexpr int SUB = P / (int)sizeof(T);      // MC: rows of the operand in one sub-block
+  static constexpr int KPB = 1024 / P;                // MC: k-rows of one load
+  static constexpr int BPS = BK / KPB;                // MC: loads of one sub-block
+  static_assert(LAY != LAY_MC || P == 256 || P == 128, "the exchange of pieces is written for these");
+  static_assert((LAY != LAY_BK && LAY != LAY_BM) || sizeof(T) == 2, "blocks are bf16");
 
-  // mc: XOR on the chunk number within LDS row k.  bf16: a read serves rows 8 g + 0..3 of two groups g
+  // MC: XOR on the chunk number within LDS row k.  bf16: a read serves rows 8 g + 0..3 of two groups g
   // with 32 bytes of each; fp32: rows 4 g + t of four groups with 64 bytes.
   static __device__ __forceinline__ uint32_t mc_swizzle(uint32_t k) {
     if (sizeof(T) == 2) {
@@ -107,74 +117,134 @@ struct Side {
     if (P == 256) return 4 * ((k >> 2) & 3);
     return 4 * ((k >> 2) & 1);
   }
-  // byte offset of the lane's 16 bytes of block b from the tile's first element; kc: chunk, its number in the slab
-  static __device__ __forceinline__ uint32_t source(int b, int lane, uint32_t ld, uint32_t* chunk) {
-    if (!MC) {
-      const uint32_t r = lane >> 2, c = (lane & 3) ^ kc_swizzle(r >> 2);
-      *chunk = c;
-      return ((uint32_t)b * 16 + r) * ld * (uint32_t)sizeof(T) + c * 16;
-    }
-    constexpr int CPR = P / 16;   // chunks of an LDS row
-    const uint32_t sub = b / BPS, k = (b % BPS) * KPB + lane / CPR;
-    const uint32_t c = (lane % CPR) ^ mc_swizzle(k);
-    return k * ld * (uint32_t)sizeof(T) + sub * P + c * 16;
+  // where the tile begins in the matrix (r0: its first row, a multiple of 32), and what a unit advances by, in bytes
+  static __device__ __forceinline__ int64_t origin(int r0, int64_t ld) {
+    if (LAY == LAY_MC) return (int64_t)r0 * (int)sizeof(T);
+    if (LAY == LAY_BM) return (int64_t)(r0 / 32) * 1024;
+    return (int64_t)r0 * ld * (int)sizeof(T);
   }
-  // the lane's part of a fragment address: rows l & 15 of a 16-row tile, elements 8 (l >> 4) .. + 7
-  // (fp32: 4 (l >> 4) .. + 3) of the slab
-  static __device__ __forceinline__ uint32_t lane_part(int lane) {
+  static __device__ __forceinline__ uint32_t step(uint32_t ld) {
+    return TURNED ? BK * ld * (uint32_t)sizeof(T) : LAY == LAY_BK ? 1024u : 64u * UNIT;
+  }
+  // byte offset of the lane's 16 bytes of block b of a unit; k: the first element of the reduction that they hold
+  // (not TURNED)
+  static __device__ __forceinline__ uint32_t source(int b, int lane, uint32_t ld, int* k) {
+    if (LAY == LAY_MC) {
+      constexpr int CPR = P / 16;   // chunks of an LDS row
+      const uint32_t sub = b / BPS, kr = (b % BPS) * KPB + lane / CPR;
+      const uint32_t c = (lane % CPR) ^ mc_swizzle(kr);
+      return kr * ld * (uint32_t)sizeof(T) + sub * P + c * 16;
+    }
+    if (LAY == LAY_BM) return (b & 1) * 16 * ld * (uint32_t)sizeof(T) + (b >> 1) * 1024 + lane * 16;
+    if (LAY == LAY_KC2) {
+      const uint32_t r = (uint32_t)b * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+      *k = (int)c * EPC;
+      return r * ld * (uint32_t)sizeof(T) + c * 16;
+    }
+    const uint32_t r = lane >> 2, c = (lane & 3) ^ kc_swizzle(r >> 2);
+    *k = (int)c * EPC;
+    if (LAY == LAY_BK) return (uint32_t)b * 16 * ld * (uint32_t)sizeof(T) + lane * 16;
+    return ((uint32_t)b * 16 + r) * ld * (uint32_t)sizeof(T) + c * 16;
+  }
+  // where a wavefront's fragments begin, from the matrix's beginning in a stage: rows l & 15 of its first 16-row
+  // tile x0 (a multiple of the number of its tiles), elements 8 (l >> 4) .. + 7 (fp32: 4 (l >> 4) .. + 3) of the slab
+  static constexpr int TPS = SUB / 16;               // MC: tiles of a sub-block
+  static constexpr uint32_t TB = 16 * sizeof(T);     // MC: bytes of a tile's piece of an LDS row
+  static __device__ __forceinline__ uint32_t first(int x0, int lane) {
     const uint32_t g = lane >> 4, j = lane & 15;
-    if (!MC) return j * 64 + ((g ^ kc_swizzle(j >> 2)) * 16);
+    if (LAY == LAY_KC || LAY == LAY_BK) return x0 * 1024 + j * 64 + ((g ^ kc_swizzle(j >> 2)) * 16);
+    if (LAY == LAY_KC2) return x0 * 2048 + j * 128 + ((g ^ ((j >> 1) & 7)) * 16);
+    if (LAY == LAY_BM) {
+      const uint32_t r = (8 * g + (j >> 2)) & 15;
+      return (x0 / 2) * 2048 + (g >> 1) * 1024 + r * 64 + ((((j & 3) >> 1) ^ kc_swizzle(r >> 2)) * 16) + (j & 1) * 8;
+    }
+    uint32_t part;
     if (sizeof(T) == 2) {
       const uint32_t k = 8 * g + (j >> 2);
-      return k * P + ((((j & 3) >> 1) ^ mc_swizzle(k)) * 16) + (j & 1) * 8;
+      part = k * P + ((((j & 3) >> 1) ^ mc_swizzle(k)) * 16) + (j & 1) * 8;
+    } else {
+      const uint32_t k = 4 * g;
+      part = k * P + (((j >> 2) ^ mc_swizzle(k)) * 16) + (j & 3) * 4;
     }
-    const uint32_t k = 4 * g;
-    return k * P + (((j >> 2) ^ mc_swizzle(k)) * 16) + (j & 3) * 4;
+    return (x0 / TPS) * (BK * P) + (part ^ ((uint32_t)(x0 % TPS) * TB));
   }
-  // where a wavefront's fragments begin, from the side's beginning in a stage: its first tile is x0, a
-  // multiple of the number of tiles it has (which divides TPS, or is a multiple of it)
-  static constexpr int TPS = SUB / 16;
-  static constexpr uint32_t TB = 16 * sizeof(T);     // mc: bytes of a tile's piece of an LDS row
-  static __device__ __forceinline__ uint32_t first(int x0, int lane) {
-    if (!MC) return x0 * 1024 + lane_part(lane);
-    return (x0 / TPS) * (BK * P) + (lane_part(lane) ^ ((uint32_t)(x0 % TPS) * TB));
-  }
-  // fragment of the tile x0 + i; at: that beginning in LDS
-  static __device__ __forceinline__ void read(Frag& f, uint32_t at, int i) {
-    if (!MC) {
-      f.u = *(lds_ptr<const u32x4_t>)(uintptr_t)(at + i * 1024);
+  // fragment of the tile x0 + i; at: that beginning in LDS; half: KC2, the slab of the pair
+  static __device__ __forceinline__ void read(Frag& f, uint32_t at, int i, int half) {
+    if (!TURNED) {
+      f.u = *(lds_ptr<const u32x4_t>)(uintptr_t)((LAY == LAY_KC2 ? at ^ (half * 64u) : at) + i * 1024 * UNIT);
       return;
     }
-    const uint32_t a = (at ^ ((uint32_t)(i % TPS) * TB)) + (i / TPS) * (BK * P);
-    if (sizeof(T) == 2) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        f.h[u] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)(a + u * 4 * P)));
+    if constexpr (sizeof(T) == 2) {
+      // (BM: four tokens on lie four rows down, with the pairs of chunks exchanged)
+      const uint32_t a0 = LAY == LAY_BM ? (at ^ ((i & 1) * 32u)) + (i / 2) * 2048 : (at ^ ((uint32_t)(i % TPS) * TB)) + (i / TPS) * (BK * P);
+      const uint32_t a1 = LAY == LAY_BM ? (at ^ ((i & 1) * 32u) ^ 288u) + (i / 2) * 2048 : a0 + 4 * P;
+      f.h[0] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)a0));
+      f.h[1] = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<s16x4_t>)(uintptr_t)a1));
     } else {
+      const uint32_t a = (at ^ ((uint32_t)(i % TPS) * TB)) + (i / TPS) * (BK * P);
 #pragma unroll
       for (int t = 0; t < 4; ++t) f.f[t] = *(lds_ptr<const float>)(uintptr_t)(a + t * P);
     }
   }
   // LDS reads of one fragment (16-byte ones are not merged; fp32 rows may be)
-  static constexpr int READS = MC ? (sizeof(T) == 2 ? 2 : 4) : 1;
+  static constexpr int READS = TURNED ? (sizeof(T) == 2 ? 2 : 4) : 1;
 };
 
-template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, bool AMC, bool BMC, int EPI>
+// The walk of one operand's loads along the reduction: the next unit within its segment, as a scalar offset from where
+// the resource begins.  Behind the last unit the resource is empty: the loads then put zeros into stages (which a
+// reduction of an odd number of slabs multiplies once), and every step issues and awaits the same number of loads.
+template <bool TWO>
+struct Walk {
+  const char *q0, *q1;   // the matrix, and that of the second segment (or, TWO, of the up columns)
+  int64_t org, bytes;
+  uint32_t unit;         // bytes of a unit's step
+  int units, reach;      // units of a segment; units that one resource serves
+  int next, todo, event; // units until the resource changes
+  uint32_t soff;
+  u32x4_t r0, r1;
+  __device__ __forceinline__ void aim() {
+    if (next == units) { next = 0; q0 = q1; }
+    const int64_t off = org + next * (int64_t)unit;
+    r0 = resource(q0 + off, todo > 0 ? bytes - off : 0);
+    if (TWO) r1 = resource(q1 + off, todo > 0 ? bytes - off : 0);
+    soff = 0;
+    // (a resource's end and a lane's offset are 32-bit: it is left behind before the scalar offset passes FAR)
+    event = todo > 0 ? min(min(todo, units - next), reach) : 0x7fffffff;
+  }
+  __device__ __forceinline__ void start(const void* p0, const void* p1, int64_t o, int64_t b, uint32_t step, int n, int at, int count) {
+    q0 = (const char*)p0; q1 = (const char*)p1;
+    org = o; bytes = b; unit = step; units = n;
+    next = at; todo = count;
+    if (next >= units) { next -= units; q0 = q1; }
+    reach = __builtin_amdgcn_readfirstlane((int)(FAR / step));
+    aim();
+  }
+  __device__ __forceinline__ void advance() {
+    ++next; --todo; soff += unit;
+    if (--event == 0) aim();
+  }
+};
+
+template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, int LA_, int LB_, int EPI>
 __global__ void __launch_bounds__(WGM* WGN * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 plain_kernel(const PlainArgs p) {
   constexpr bool PAIR = EPI == EPI_GLU;
   constexpr int NW = WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
   constexpr int BNH = PAIR ? BN / 2 : BN;      // output columns of the tile
-  using SA = Side<T, BM, AMC>;
-  using SB = Side<T, BNH, BMC>;
+  using SA = Side<T, BM, LA_>;
+  using SB = Side<T, BNH, LB_>;
   constexpr int BK = SA::BK;
-  constexpr int A_BLK = BM / 16, B_BLK = BN / 16, HB = BNH / 16;   // HB: blocks of one matrix's columns
-  constexpr int LA = A_BLK / NW, LB = B_BLK / NW, LPW = LA + LB;
-  constexpr int STAGE = (A_BLK + B_BLK) * 1024;
+  constexpr int A_BLK = BM / 16, B_BLK = BN / 16, HB = BNH / 16;   // blocks of a slab; HB: of one matrix's columns
+  constexpr int LA = A_BLK / NW, LB = B_BLK / NW, LPW = LA + LB;   // loads of a wavefront and slab
+  // a ring of STAGES slabs; pairs of slabs: one more pair
+  constexpr bool PAIRED = SA::UNIT == 2 || SB::UNIT == 2;
+  constexpr int NA = SA::UNIT == 2 ? STAGES / 2 + 1 : STAGES, NB = SB::UNIT == 2 ? STAGES / 2 + 1 : STAGES;
+  constexpr int UA = SA::UNIT_BYTES, UB = SB::UNIT_BYTES * (PAIR ? 2 : 1), B_AT = NA * UA;
   static_assert(A_BLK % NW == 0 && B_BLK % NW == 0, "blocks divide over the wavefronts");
   static_assert(!PAIR || HB % NW == 0 || NW % HB == 0, "a load belongs to one matrix");
-  static_assert(STAGES >= 3 && STAGES * LPW <= 63, "loads in flight must fit the counter");
+  static_assert(!PAIR || SB::UNIT == 1, "two matrices are fetched slab by slab");
+  static_assert(STAGES >= 3 && (!PAIRED || STAGES % 2 == 0) && (STAGES + 1) * LPW <= 63, "loads in flight must fit the counter");
   static_assert(TM % 2 == 0 && (!PAIR || TN % 2 == 0), "row tiles are stored in pairs");
 
   extern __shared__ u32x4_t smem_v[];
@@ -193,65 +263,45 @@ plain_kernel(const PlainArgs p) {
   const int which = tn2 >= tiles_n1, tn = which ? tn2 - tiles_n1 : tn2;
   const int m0 = tm * BM, n0 = tn * BNH;
 
-  // slabs: segs times ceil(K / BK); this range's part of them
-  const int ns = (p.K + BK - 1) / BK;
+  // slabs: segs times ceil(K / BK), a whole number of pairs of them if pairs are fetched; this range's part
+  constexpr int CUT = PAIRED ? 2 : 1;
+  const int ns = (p.K + BK * CUT - 1) / (BK * CUT) * CUT;
   const int total = ns * p.segs;
-  const int per = (total + p.n_split - 1) / p.n_split;
+  const int per = (total / CUT + p.n_split - 1) / p.n_split * CUT;
   const int s0 = blockIdx.y * per;
   const int nk = max(0, min(total, s0 + per) - s0);
-  const int k_end = (p.K + SA::EPC - 1) / SA::EPC * SA::EPC;   // kc: chunks from here on read as zero
+  const int k_end = (p.K + SA::EPC - 1) / SA::EPC * SA::EPC;   // chunks of the reduction from here on read as zero
 
-  uint32_t va[LA], vb[LB], chunk = 0;
+  uint32_t va[SA::UNIT][LA], vb[SB::UNIT][LB];
+  int ka0 = 0, kb0 = 0;   // the lane's first element in a unit (the same for all its blocks)
 #pragma unroll
-  for (int i = 0; i < LA; ++i) va[i] = SA::source(wave + i * NW, lane, (uint32_t)p.lda, &chunk);
+  for (int h = 0; h < SA::UNIT; ++h)
 #pragma unroll
-  for (int i = 0; i < LB; ++i) vb[i] = SB::source((wave + i * NW) % HB, lane, (uint32_t)p.ldb, &chunk);
-  const int64_t a_org = (AMC ? (int64_t)m0 : (int64_t)m0 * p.lda) * (int)sizeof(T);
-  const int64_t b_org = (BMC ? (int64_t)n0 : (int64_t)n0 * p.ldb) * (int)sizeof(T);
-  const uint32_t a_step = AMC ? BK * (uint32_t)p.lda * (uint32_t)sizeof(T) : 64, b_step = BMC ? BK * (uint32_t)p.ldb * (uint32_t)sizeof(T) : 64;
+    for (int i = 0; i < LA; ++i) va[h][i] = SA::source(wave + i * NW + h * A_BLK, lane, (uint32_t)p.lda, &ka0);
+#pragma unroll
+  for (int h = 0; h < SB::UNIT; ++h)
+#pragma unroll
+    for (int i = 0; i < LB; ++i) vb[h][i] = SB::source((wave + i * NW) % HB + h * HB, lane, (uint32_t)p.ldb, &kb0);
   const uint32_t lds0 = lds_offset((const char*)smem);
-  const uint32_t st0 = lds0 + wave * 1024;
-  // kc: the chunks behind the reduction's end, in the last slab of a segment
-  const uint32_t beyond = (!AMC || !BMC) && (ns - 1) * BK + (int)chunk * SA::EPC >= k_end ? NOWHERE : 0u;
+  const uint32_t lds_w = lds0 + wave * 1024;
+  Walk<false> wa;
+  Walk<PAIR> wb;
+  wa.start(p.A[0], p.A[1], SA::origin(m0, p.lda), p.a_bytes, SA::step((uint32_t)p.lda), ns / SA::UNIT, s0 / SA::UNIT, nk / SA::UNIT);
+  wb.start(which ? p.B[1] : p.B[0], p.B[1], SB::origin(n0, p.ldb), p.b_bytes, SB::step((uint32_t)p.ldb), ns / SB::UNIT,
+           s0 / SB::UNIT, nk / SB::UNIT);
 
-  // The slab whose loads go out next: its number within its segment, and scalar offsets from where the
-  // resources begin.  Behind the last slab the resources are empty: the loads then put zeros into stages
-  // (which a reduction of an odd number of slabs multiplies once), and every step issues and awaits the same
-  // number of loads.
-  int next = s0, seg = 0;
-  if (s0 >= ns) { next -= ns; seg = 1; }   // (segs = 2)
-  int todo = nk, event = 0;                // slabs still to be loaded, and until the resources change
-  const int reach = __builtin_amdgcn_readfirstlane((int)(FAR / max(a_step, b_step)));
-  u32x4_t ra, rb0, rb1;
-  uint32_t sa = 0, sb = 0;
-  auto aim = [&]() {
-    if (next == ns) { next = 0; seg = 1; }
-    const int64_t ao = a_org + next * (int64_t)a_step, bo = b_org + next * (int64_t)b_step;
-    ra = resource((const char*)(seg ? p.A[1] : p.A[0]) + ao, todo > 0 ? p.a_bytes - ao : 0);
-    rb0 = resource((const char*)((seg | which) ? p.B[1] : p.B[0]) + bo, todo > 0 ? p.b_bytes - bo : 0);
-    if (PAIR) rb1 = resource((const char*)p.B[1] + bo, todo > 0 ? p.b_bytes - bo : 0);
-    sa = 0; sb = 0;
-    // (a resource's end and a lane's offset are 32-bit: it is left behind before the scalar offset passes FAR)
-    event = todo > 0 ? min(min(todo, ns - next), reach) : 0x7fffffff;
+  // load number i of the left (right) operand's next unit into a stage; half: KC2, which half of its rows
+  auto load_a = [&](int i, int stage, int half) {
+    const uint32_t out = !SA::TURNED && ka0 >= k_end - wa.next * (BK * SA::UNIT) ? NOWHERE : 0u;
+    load_to_lds(wa.r0, lds_w + stage * UA + (half * A_BLK + i * NW) * 1024, SA::TURNED ? va[half][i] : va[half][i] | out, wa.soff);
   };
-  // load number i of that slab into a stage
-  auto issue = [&](int i, int stage) {
-    const uint32_t st = st0 + stage * STAGE;
-    const uint32_t out = next == ns - 1 ? beyond : 0u;
-    if (i < LA) {
-      load_to_lds(ra, st + i * NW * 1024, AMC ? va[i] : va[i] | out, sa);
-    } else {
-      const int b = i - LA;
-      // (gated: load b NW + wave belongs to the second matrix from HB on)
-      const bool second = PAIR && (HB >= NW ? b * NW >= HB : (wave + b * NW) >= HB);
-      load_to_lds(second ? rb1 : rb0, st + (A_BLK + b * NW) * 1024, BMC ? vb[b] : vb[b] | out, sb);
-    }
+  auto load_b = [&](int i, int stage, int half) {
+    const uint32_t out = !SB::TURNED && kb0 >= k_end - wb.next * (BK * SB::UNIT) ? NOWHERE : 0u;
+    // (gated: load i NW + wave belongs to the second matrix from HB on)
+    const bool second = PAIR && (HB >= NW ? i * NW >= HB : (wave + i * NW) >= HB);
+    load_to_lds(second ? wb.r1 : wb.r0, lds_w + B_AT + stage * UB + (half * HB + i * NW) * 1024,
+                SB::TURNED ? vb[half][i] : vb[half][i] | out, wb.soff);
   };
-  auto advance = [&]() {
-    ++next; --todo; sa += a_step; sb += b_step;
-    if (--event == 0) aim();
-  };
-  aim();
 
   f32x4_t acc[TM][TN];
 #pragma unroll
@@ -260,12 +310,14 @@ plain_kernel(const PlainArgs p) {
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   constexpr int TNH = PAIR ? TN / 2 : TN;   // column tiles of one matrix
-  const uint32_t la = lds0 + SA::first(wm * TM, lane), lb = lds0 + A_BLK * 1024 + SB::first(wn * TNH, lane);
+  const uint32_t la = lds0 + SA::first(wm * TM, lane), lb = lds0 + B_AT + SB::first(wn * TNH, lane);
   // DBL: the left operand's fragments in two sets as well
   constexpr bool DBL = TM * TN <= 16;
   Frag fa[DBL ? 2 : 1][TM], fb[2][TN];
-  auto read_a = [&](int set, int i, uint32_t st) { SA::read(fa[DBL ? set : 0][i], la + st, i); };
-  auto read_b = [&](int set, int j, uint32_t st) { SB::read(fb[set][j], lb + st + (j / TNH) * HB * 1024, j % TNH); };
+  auto read_a = [&](int set, int i, uint32_t st, int half) { SA::read(fa[DBL ? set : 0][i], la + st, i, half); };
+  auto read_b = [&](int set, int j, uint32_t st, int half) {
+    SB::read(fb[set][j], lb + st + (j / TNH) * (HB * 1024), j % TNH, half);
+  };
   auto mma = [&](int set, int i, int j) {
     if constexpr (sizeof(T) == 2) {
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][j].v, fa[DBL ? set : 0][i].v, acc[i][j], 0, 0, 0);
@@ -282,30 +334,61 @@ plain_kernel(const PlainArgs p) {
   //     the loads of slab s + 1 + STAGES go out behind it.
   //   otherwise: the left operand's fragment i is overwritten as soon as the MFMAs that use it are issued; the
   //     barrier in the middle retires slab s and publishes slab s + 2; the loads of slab s + STAGES follow.
+  // An operand fetched in pairs of slabs retires a pair in every second step, and half of the rows of the next
+  // pair go out in each: one half is under way before the first step, and then a pair is as many steps under
+  // way as a slab.
 #pragma unroll
-  for (int s = 0; s < STAGES; ++s) {
+  for (int m = 0; m < STAGES + (PAIRED ? 1 : 0); ++m) {
+    const int t = PAIRED ? m - 1 : m;   // slab
+    if (SA::UNIT == 2) {
 #pragma unroll
-    for (int i = 0; i < LPW; ++i) issue(i, s);
-    advance();
+      for (int i = 0; i < LA; ++i) load_a(i, m / 2, m & 1);
+      if (m & 1) wa.advance();
+    } else if (t >= 0) {
+#pragma unroll
+      for (int i = 0; i < LA; ++i) load_a(i, t, 0);
+      wa.advance();
+    }
+    if (SB::UNIT == 2) {
+#pragma unroll
+      for (int i = 0; i < LB; ++i) load_b(i, m / 2, m & 1);
+      if (m & 1) wb.advance();
+    } else if (t >= 0) {
+#pragma unroll
+      for (int i = 0; i < LB; ++i) load_b(i, t, 0);
+      wb.advance();
+    }
   }
   wait_vmcnt<(STAGES - 2) * LPW>();   // slabs 0 and 1
   lds_barrier();
 #pragma unroll
-  for (int j = 0; j < TN; ++j) read_b(0, j, 0);
+  for (int j = 0; j < TN; ++j) read_b(0, j, 0, 0);
 #pragma unroll
-  for (int i = 0; i < TM; ++i) read_a(0, i, 0);
+  for (int i = 0; i < TM; ++i) read_a(0, i, 0, 0);
   if (DBL) {
     wait_lgkmcnt<0>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < LPW; ++i) issue(i, 0);
-    advance();
+    for (int i = 0; i < LA; ++i) load_a(i, SA::UNIT == 2 ? NA - 1 : 0, SA::UNIT == 2);
+    wa.advance();
+#pragma unroll
+    for (int i = 0; i < LB; ++i) load_b(i, SB::UNIT == 2 ? NB - 1 : 0, SB::UNIT == 2);
+    wb.advance();
   }
-  int stage = 0;   // stage of slab s
+  int sta = 0, stb = 0;   // the stages of slab s
   auto step = [&](auto setc) {
-    constexpr int set = decltype(setc)::value;
-    const int ns1 = stage + 1 == STAGES ? 0 : stage + 1;
-    const uint32_t nx = ns1 * STAGE;
+    constexpr int set = decltype(setc)::value;   // s mod 2
+    const int na = sta + 1 == NA ? 0 : sta + 1, nb = stb + 1 == NB ? 0 : stb + 1;
+    // where slab s + 1 is read, and where the loads of this step go
+    const uint32_t xa = (SA::UNIT == 2 && set == 0 ? sta : na) * UA, xb = (SB::UNIT == 2 && set == 0 ? stb : nb) * UB;
+    const int ha = SA::UNIT == 2 && set == 0, hb = SB::UNIT == 2 && set == 0;
+    const int pa = SA::UNIT == 2 ? (!DBL && set == 0 ? (sta == 0 ? NA - 1 : sta - 1) : sta) : DBL ? na : sta;
+    const int pb = SB::UNIT == 2 ? (!DBL && set == 0 ? (stb == 0 ? NB - 1 : stb - 1) : stb) : DBL ? nb : stb;
+    constexpr int ga = SA::UNIT == 2 ? (DBL ? set : 1 - set) : 0, gb = SB::UNIT == 2 ? (DBL ? set : 1 - set) : 0;
+    auto issue = [&](int l) {
+      if (l < LA) load_a(l, pa, ga);
+      else load_b(l - LA, pb, gb);
+    };
     FFS_ORDER;
     if constexpr (DBL) {
       constexpr int NM = TM * TN, NR = TM + TN, RD = NM * 5 / 8, SYNC = NM * 3 / 4;
@@ -317,8 +400,8 @@ plain_kernel(const PlainArgs p) {
 #pragma unroll
         for (int r = 0; r < NR; ++r)
           if (r * RD / NR == q) {
-            if (r < TN) read_b(set ^ 1, r, nx);
-            else read_a(set ^ 1, r - TN, nx);
+            if (r < TN) read_b(set ^ 1, r, xb, hb);
+            else read_a(set ^ 1, r - TN, xa, ha);
           }
         FFS_ORDER;
         if (q == SYNC - 1) {
@@ -329,7 +412,7 @@ plain_kernel(const PlainArgs p) {
         }
 #pragma unroll
         for (int l = 0; l < LPW; ++l)
-          if (SYNC + l * (NM - SYNC) / LPW == q) issue(l, ns1);
+          if (SYNC + l * (NM - SYNC) / LPW == q) issue(l);
         FFS_ORDER;
       }
     } else {
@@ -344,10 +427,10 @@ plain_kernel(const PlainArgs p) {
           FFS_ORDER;
 #pragma unroll
           for (int q = 0; q < TN; ++q)
-            if (q * TM == i * TN + jj) read_b(set ^ 1, q, nx);
+            if (q * TM == i * TN + jj) read_b(set ^ 1, q, xb, hb);
           FFS_ORDER;
         }
-        read_a(0, i, nx);
+        read_a(0, i, xa, ha);
         FFS_ORDER;
         if (i == RB) {
           wait_vmcnt<(STAGES - 3) * LPW>();
@@ -358,13 +441,15 @@ plain_kernel(const PlainArgs p) {
         if (i > RB) {
 #pragma unroll
           for (int l = 0; l < LPW; ++l)
-            if (l * (TM - RB - 1) / LPW == i - RB - 1) issue(l, stage);
+            if (l * (TM - RB - 1) / LPW == i - RB - 1) issue(l);
           FFS_ORDER;
         }
       }
     }
-    advance();
-    stage = ns1;
+    if (SA::UNIT == 1 || ga == 1) wa.advance();
+    if (SB::UNIT == 1 || gb == 1) wb.advance();
+    if (SA::UNIT == 1 || set == 1) sta = na;
+    if (SB::UNIT == 1 || set == 1) stb = nb;
   };
   for (int s = 0; s < nk; s += 2) {
     step(std::integral_constant<int, 0>{});
@@ -379,12 +464,13 @@ plain_kernel(const PlainArgs p) {
   constexpr int OW = PAIR ? WN / 2 : WN;             // output columns of a wavefront
   constexpr int LPR = OW / 8, RP = 64 / LPR, NP = 32 / RP;
   constexpr int PITCH = WN * 4 + 16;
-  static_assert(NW * 32 * PITCH <= STAGES * STAGE, "the stages' memory is used");
+  static_assert(NW * 32 * PITCH <= B_AT + NB * UB, "the stages' memory is used");
   wait_lgkmcnt<0>();
   lds_barrier();   // every wavefront is done with the stages
   char* const own = smem + wave * (32 * PITCH);
   const int col = n0 + wn * OW + (lane % LPR) * 8;
   const int64_t row0 = m0 + wm * WM + lane / LPR;
+  const int rows = stored_rows<T, EPI>(p);
   using KT = kept_t<T>;
   Raw8<KT> ka[2][EPI == EPI_GRAD ? NP : 1], kb[2][EPI == EPI_GRAD ? NP : 1];
   auto fetch = [&](int set, int ip) {
@@ -392,7 +478,7 @@ plain_kernel(const PlainArgs p) {
 #pragma unroll
       for (int q = 0; q < NP; ++q) {
         const int64_t row = row0 + ip * 16 + q * RP;
-        if (row < p.M && col < p.n_store && p.part == nullptr) {
+        if (row < rows && col < p.n_store && p.part == nullptr) {
           ka[set][q].load(p.D1, row * p.ldi + col);
           if (p.D2 != nullptr) kb[set][q].load(p.D2, row * p.ldi + col);
         }
@@ -416,7 +502,7 @@ plain_kernel(const PlainArgs p) {
       load8<float>(at, 0, v);
       if (PAIR) load8<float>(at + OW * 4, 0, u);
       const int64_t row = row0 + ip * 16 + q * RP;
-      if (row >= p.M || col >= p.n_store) continue;
+      if (row >= (p.part != nullptr ? p.M : rows) || col >= p.n_store) continue;
       if (p.part != nullptr) {
         const int planes = PAIR || p.twin ? 2 : 1;
         const int64_t to = (((int64_t)blockIdx.y * planes + which) * p.M + row) * p.ldp + col;
@@ -426,7 +512,7 @@ plain_kernel(const PlainArgs p) {
         float a[8], b[8];
         ka[(ip / 2) & 1][q].get(a);
         kb[(ip / 2) & 1][q].get(b);
-        grad8<T>(p, row * p.ldi + col, col, v, a, b);
+        grad8<T>(p, row, col, v, a, b);
       } else {
         emit8<T, EPI>(p, which, row, col, v, u);
       }
@@ -441,7 +527,7 @@ __global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
   constexpr bool PAIR = EPI == EPI_GLU;
   const int cpr = p.n_store / 8;
   const int64_t id = (int64_t)blockIdx.x * 64 + threadIdx.x;
-  const int64_t per_plane = (int64_t)p.M * cpr;
+  const int64_t per_plane = (int64_t)stored_rows<T, EPI>(p) * cpr;
   const int which = p.twin && id >= per_plane;
   const int64_t in = which ? id - per_plane : id;
   if (in >= per_plane) return;
@@ -450,7 +536,7 @@ __global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
   const int planes = PAIR || p.twin ? 2 : 1;
   const int64_t plane = (int64_t)p.M * p.ldp;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int s0 = 0; s0 < p.n_split; s0 += 4) {
+  for (int s0 = 0; row < p.M && s0 < p.n_split; s0 += 4) {
     float w[4][8], x[PAIR ? 4 : 1][8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -485,11 +571,12 @@ __global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* s
   }
 }
 
-template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, bool AMC, bool BMC, int EPI>
+template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, int LA_, int LB_, int EPI>
 static int launch_tile(const PlainArgs& a, hipStream_t st) {
-  constexpr size_t lds = (size_t)STAGES * (BM + BN) * 64;
+  constexpr auto ring = [](int rows, int lay) { return (size_t)rows * (lay == LAY_KC2 ? (STAGES / 2 + 1) * 128 : STAGES * 64); };
+  constexpr size_t lds = ring(BM, LA_) + ring(BN, LB_);
   static_assert(lds <= 160 * 1024, "LDS budget of a CU");
-  auto kern = plain_kernel<T, BM, BN, WGM, WGN, STAGES, AMC, BMC, EPI>;
+  auto kern = plain_kernel<T, BM, BN, WGM, WGN, STAGES, LA_, LB_, EPI>;
   // (a set-once note per device that the limit of dynamic LDS has been raised; racing first calls both
   // set it, which is harmless)
   static std::atomic<uint64_t> configured{0};
@@ -513,7 +600,7 @@ static int launch_tile(const PlainArgs& a, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_128x256 = 3, PS_SHAPES = 4 };
+enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_SHAPES = 3 };
 struct Plan { int shape, split; };
 
 // Choice of the tile and of the ranges that the reduction is cut into, by estimated time (us): t[k - 1] a slab with k
@@ -524,9 +611,8 @@ struct Plan { int shape, split; };
 struct ShapeCost { int bm, bn, per_cu; float t[4], fixed; };
 static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.246f, 0.452f}, 4.9f},
                                                 {256, 256, 1, {0.514f}, 7.0f},
-                                                {64, 64, 4, {0.138f, 0.227f, 0.497f, 0.546f}, 3.9f},
-                                                {128, 256, 2, {0.500f, 0.704f}, 5.6f}};
-static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {1.05f, 1.61f}, 1.6f}, {}, {64, 64, 4, {0.348f, 0.570f, 0.989f, 1.21f}, 0.3f}, {}};
+                                                {64, 64, 4, {0.138f, 0.227f, 0.497f, 0.546f}, 3.9f}};
+static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {1.05f, 1.61f}, 1.6f}, {}, {64, 64, 4, {0.348f, 0.570f, 0.989f, 1.21f}, 0.3f}};
 struct ProductCost {
   float layout[3];        // factor of a slab: right operand mc, both kc, both mc
   float bw, overlap;      // bytes a us, and the share of the traffic's time that comes on top
@@ -536,11 +622,13 @@ static const ProductCost COST_BF16 = {{1.0f, 1.08f, 1.17f}, 4.55e6f, 0.2f, 1.0f,
 static const ProductCost COST_F32 = {{1.0f, 0.98f, 1.06f}, 2.04e6f, 0.22f, 1.6f, 0.26f, 1.91e6f};
 constexpr size_t PART_ROOM = (size_t)32 << 20;   // scratch for ranges' sums
 
+static inline bool turned(int lay) { return lay == LAY_MC || lay == LAY_BM; }
+
 static Plan plain_plan(const PlainArgs& a, int epi, int bf16) {
   const ProductCost& c = bf16 ? COST_BF16 : COST_F32;
   const int esz = bf16 ? 2 : 4, planes = epi == EPI_GLU || a.twin ? 2 : 1;
   const int bk = bf16 ? 32 : 16, slabs = a.segs * ((a.K + bk - 1) / bk);
-  const float layout = c.layout[a.a_mc ? 2 : a.b_mc ? 0 : 1];
+  const float layout = c.layout[turned(a.a_lay) ? 2 : turned(a.b_lay) ? 0 : 1];
   const int stored = epi == EPI_GLU ? 3 : epi == EPI_GELU ? 2 : epi == EPI_GRAD ? (a.D2 ? 4 : 2) : planes;
   const float bytes = (float)esz * ((float)a.M * a.K * a.segs + (float)a.N * a.K * (planes > a.segs ? planes : a.segs) +
                                     (float)stored * a.M * a.N);
@@ -567,48 +655,50 @@ static Plan plain_plan(const PlainArgs& a, int epi, int bf16) {
   return best;
 }
 
-template <typename T, bool AMC, bool BMC, int EPI>
+template <typename T, int LA_, int LB_, int EPI>
 static int launch_shape(const PlainArgs& a, int shape, hipStream_t st) {
-  constexpr bool BF = sizeof(T) == 2;
+  constexpr bool BF = sizeof(T) == 2, PAIRED = LA_ == LAY_KC2 || LB_ == LAY_KC2;
+  if (a.a_lay != LA_ || a.b_lay != LB_) return -1;
   switch (shape) {
-    case PS_128x128: return launch_tile<T, 128, 128, 2, 2, 5, AMC, BMC, EPI>(a, st);
+    case PS_128x128: return launch_tile<T, 128, 128, 2, 2, PAIRED ? 4 : 5, LA_, LB_, EPI>(a, st);
     case PS_64x64:   // (bf16 gated: 64 x 64 of each matrix)
-      return BF && EPI == EPI_GLU ? launch_tile<T, 64, 128, 2, 2, 6, AMC, BMC, EPI>(a, st)
-                                  : launch_tile<T, 64, BF && EPI == EPI_GLU ? 128 : 64, 2, 2, 8, AMC, BMC, EPI>(a, st);
+      return launch_tile<T, 64, BF && EPI == EPI_GLU ? 128 : 64, 2, 2, BF && EPI == EPI_GLU ? 6 : 8, LA_, LB_, EPI>(a, st);
   }
   if constexpr (BF) {
-    if (shape == PS_256x256) return launch_tile<T, 256, 256, 2, 4, 4, AMC, BMC, EPI>(a, st);
-    if (shape == PS_128x256) return launch_tile<T, 128, 256, 1, 4, 3, AMC, BMC, EPI>(a, st);
+    if (shape == PS_256x256) return launch_tile<T, 256, 256, 2, 4, 4, LA_, LB_, EPI>(a, st);
   }
   return -1;
 }
 
 template <typename T, int EPI>
 static int launch_reduce(const PlainArgs& a, hipStream_t st) {
-  const int64_t n = (int64_t)a.M * (a.n_store / 8) * (a.twin ? 2 : 1);
+  const int64_t n = (int64_t)stored_rows<T, EPI>(a) * (a.n_store / 8) * (a.twin ? 2 : 1);
   hipLaunchKernelGGL((plain_reduce_kernel<T, EPI>), dim3((unsigned)((n + 63) / 64)), dim3(64), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
+template <typename T, int LA_, int LB_, int EPI>
+static int launch_whole(const PlainArgs& a, int shape, hipStream_t st) {
+  const int rc = launch_shape<T, LA_, LB_, EPI>(a, shape, st);
+  return rc == 0 && a.part ? launch_reduce<T, EPI>(a, st) : rc;
+}
+
+// The products of the two passes and the way their operands lie.
 template <typename T>
 static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) {
-  int rc = -1;
-  if (epi == EPI_OUT) {
-    if (!a.a_mc && a.b_mc) rc = launch_shape<T, false, true, EPI_OUT>(a, shape, st);
-    else if (!a.a_mc && !a.b_mc) rc = launch_shape<T, false, false, EPI_OUT>(a, shape, st);
-    else if (a.a_mc && a.b_mc) rc = launch_shape<T, true, true, EPI_OUT>(a, shape, st);
-    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_OUT>(a, st);
-  } else if (epi == EPI_GLU && !a.a_mc && a.b_mc) {
-    rc = launch_shape<T, false, true, EPI_GLU>(a, shape, st);
-    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GLU>(a, st);
-  } else if (epi == EPI_GELU && !a.a_mc && a.b_mc) {
-    rc = launch_shape<T, false, true, EPI_GELU>(a, shape, st);
-    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GELU>(a, st);
-  } else if (epi == EPI_GRAD && !a.a_mc && !a.b_mc) {
-    rc = launch_shape<T, false, false, EPI_GRAD>(a, shape, st);
-    if (rc == 0 && a.part) rc = launch_reduce<T, EPI_GRAD>(a, st);
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int ACT_K = BF ? LAY_BK : LAY_KC2, ACT_M = BF ? LAY_BM : LAY_MC;   // this path's activations
+  switch (epi) {
+    case EPI_GLU: return launch_whole<T, LAY_KC2, LAY_MC, EPI_GLU>(a, shape, st);
+    case EPI_GELU: return launch_whole<T, LAY_KC2, LAY_MC, EPI_GELU>(a, shape, st);
+    case EPI_GRAD: return launch_whole<T, LAY_KC2, LAY_KC, EPI_GRAD>(a, shape, st);
+    case EPI_OUT:
+      if (!turned(a.a_lay) && turned(a.b_lay)) return launch_whole<T, ACT_K, LAY_MC, EPI_OUT>(a, shape, st);        // H W2
+      if (!turned(a.a_lay)) return launch_whole<T, ACT_K, BF ? LAY_KC2 : LAY_KC, EPI_OUT>(a, shape, st);            // dU W1^T
+      if (a.a_lay == LAY_MC) return launch_whole<T, LAY_MC, ACT_M, EPI_OUT>(a, shape, st);                          // X^T dU
+      return launch_whole<T, ACT_M, LAY_MC, EPI_OUT>(a, shape, st);                                                 // H^T dY
   }
-  return rc;
+  return -1;
 }
 
 size_t plain_part_room() { return PART_ROOM; }

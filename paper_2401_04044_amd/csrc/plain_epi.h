@@ -102,9 +102,20 @@ __device__ __forceinline__ void store1(void* base, int64_t at, bool f32, float v
   else ((bf16_t*)base)[at] = f32_to_bf16(v);
 }
 
+// where an activation's element lies, and how many rows of it are stored
+template <typename T>
+__device__ __forceinline__ int64_t act_at(int64_t row, int col, int64_t ldi) {
+  return sizeof(T) == 2 ? blocked_at(row, col, ldi) : row * ldi + col;
+}
+template <typename T, int EPI>
+inline __host__ __device__ int stored_rows(const PlainArgs& p) {
+  return sizeof(T) == 2 && EPI != EPI_OUT ? (p.M + 15) / 16 * 16 : p.M;
+}
+
 // EPI_GRAD: dH in v, the kept derivatives in a and b
 template <typename T>
-__device__ __forceinline__ void grad8(const PlainArgs& p, int64_t at, int col, const float (&v)[8], float (&a)[8], float (&b)[8]) {
+__device__ __forceinline__ void grad8(const PlainArgs& p, int64_t row, int col, const float (&v)[8], float (&a)[8], float (&b)[8]) {
+  const int64_t at = act_at<T>(row, col, p.ldi);
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = col + e < p.N ? v[e] * a[e] : 0.f;
   store8<T>(p.O1, at, a);
@@ -154,7 +165,7 @@ __device__ __forceinline__ void emit8(const PlainArgs& p, int which, int64_t row
   if (EPI == EPI_GRAD) {
     load8<kept_t<T>>(p.D1, at, a);
     if (p.D2 != nullptr) load8<kept_t<T>>(p.D2, at, b);
-    grad8<T>(p, at, col, v, a, b);
+    grad8<T>(p, row, col, v, a, b);
     return;
   }
   float h[8];
@@ -170,7 +181,7 @@ __device__ __forceinline__ void emit8(const PlainArgs& p, int which, int64_t row
     }
     if (col + e >= p.N) { h[e] = 0.f; a[e] = 0.f; b[e] = 0.f; }
   }
-  store8<T>(p.H, at, h);
+  store8<T>(p.H, act_at<T>(row, col, p.ldi), h);
   if (p.D1 != nullptr) {
     store8<kept_t<T>>((void*)p.D1, at, a);
     if (EPI == EPI_GLU) store8<kept_t<T>>((void*)p.D2, at, b);

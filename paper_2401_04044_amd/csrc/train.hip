@@ -35,7 +35,8 @@ int check_dense(const ffsplit_desc_t* d, int64_t T) {
 struct Dense {
   int bf16, gated, d, f, f8, ldi, planes;
   int64_t T, esz;
-  size_t act_bytes;      // of H, D1, D2, dU or dG: [T, ldi]
+  int64_t rows;          // of the activations below: T, in bf16 rounded up to the blocks' 16
+  size_t act_bytes;      // of H, D1, D2, dU or dG: [rows, ldi]
   size_t pad_bytes;      // of an aligned copy of W1 or Wg (0: rows are aligned as they are)
 };
 
@@ -46,7 +47,8 @@ Dense dense_of(const ffsplit_desc_t& d, int64_t T) {
   s.planes = s.gated ? 2 : 1;
   s.d = d.d_model; s.f = d.d_ff; s.f8 = round_up(d.d_ff, 8); s.ldi = round_up(d.d_ff, 64);
   s.T = T; s.esz = s.bf16 ? 2 : 4;
-  s.act_bytes = align256((size_t)T * s.ldi * s.esz);
+  s.rows = s.bf16 ? (T + 15) / 16 * 16 : T;
+  s.act_bytes = align256((size_t)s.rows * s.ldi * s.esz);
   s.pad_bytes = s.f8 == s.f ? 0 : align256((size_t)s.d * s.f8 * s.esz);
   return s;
 }
@@ -74,10 +76,16 @@ PlainArgs product(int64_t M, int N, int64_t K) {
   PlainArgs a = {};
   a.M = (int)M; a.N = N; a.K = (int)K; a.n_store = round_up(N, 8);
   a.segs = 1;
+  a.a_lay = LAY_KC2; a.b_lay = LAY_MC;
   return a;
 }
-// bytes of a stored operand: rows of len elements, ld apart
+// bytes of a row-major operand: rows of len elements, ld apart
 inline int64_t extent(int64_t rows, int64_t ld, int64_t len, int64_t esz) { return ((rows - 1) * ld + len) * esz; }
+
+// an activation's layout with the reduction over the neurons or the tokens, and its bytes
+inline int act_k(const Dense& s) { return s.bf16 ? LAY_BK : LAY_KC2; }
+inline int act_m(const Dense& s) { return s.bf16 ? LAY_BM : LAY_MC; }
+inline int64_t act_extent(const Dense& s) { return s.bf16 ? s.rows * s.ldi * s.esz : extent(s.T, s.ldi, s.f8, s.esz); }
 
 int dense_forward(const Dense& s, const void* X, const void* W1, const void* Wg, const void* W2, void* Y,
                   const float* residual, int y_f32, void* kept, char* ws, hipStream_t st) {
@@ -89,13 +97,13 @@ int dense_forward(const Dense& s, const void* X, const void* W1, const void* Wg,
   float* const part = (float*)at;
   PlainArgs a = product(s.T, s.f, s.d);
   a.A[0] = X; a.lda = s.d; a.a_bytes = extent(s.T, s.d, s.d, s.esz);
-  a.B[0] = s.gated ? g : u; a.B[1] = u; a.ldb = s.f8; a.b_mc = 1; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
+  a.B[0] = s.gated ? g : u; a.B[1] = u; a.ldb = s.f8; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
   a.H = H; a.ldi = s.ldi;
   if (kept) { a.D1 = H + s.act_bytes; a.D2 = H + 2 * s.act_bytes; }
   if (launch_plain(a, s.gated ? EPI_GLU : EPI_GELU, s.bf16, part, st)) return -1;
   a = product(s.T, s.d, s.f);
-  a.A[0] = H; a.lda = s.ldi; a.a_bytes = extent(s.T, s.ldi, s.f8, s.esz);
-  a.B[0] = W2; a.ldb = s.d; a.b_mc = 1; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
+  a.A[0] = H; a.lda = s.ldi; a.a_lay = act_k(s); a.a_bytes = act_extent(s);
+  a.B[0] = W2; a.ldb = s.d; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
   a.C[0] = Y; a.ldc = s.d; a.resid = residual; a.out_f32 = y_f32;
   return launch_plain(a, EPI_OUT, s.bf16, part, st);
 }
@@ -111,13 +119,13 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   at += s.planes * s.act_bytes;
   float* const part = (float*)at;
   const char* const H = (const char*)kept;
-  const int64_t act_ext = extent(s.T, s.ldi, s.f8, s.esz), x_ext = extent(s.T, s.d, s.d, s.esz);
+  const int64_t act_ext = act_extent(s), x_ext = extent(s.T, s.d, s.d, s.esz);
   PlainArgs a;
   if (dX || dW1 || dWg) {
     // dU = (dY W2^T) D1, dG = (dY W2^T) D2
     a = product(s.T, s.f, s.d);
     a.A[0] = dY; a.lda = s.d; a.a_bytes = x_ext;
-    a.B[0] = W2; a.ldb = s.d; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
+    a.B[0] = W2; a.ldb = s.d; a.b_lay = LAY_KC; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
     a.D1 = H + s.act_bytes; a.O1 = dU; a.ldi = s.ldi;
     if (s.gated) { a.D2 = H + 2 * s.act_bytes; a.O2 = dG; }
     if (launch_plain(a, EPI_GRAD, s.bf16, part, st)) return -1;
@@ -125,8 +133,8 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   if (dX) {
     // dX = dU W1^T + dG Wg^T
     a = product(s.T, s.d, s.f);
-    a.A[0] = dU; a.A[1] = dG; a.lda = s.ldi; a.a_bytes = act_ext;
-    a.B[0] = u; a.B[1] = g; a.ldb = s.f8; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
+    a.A[0] = dU; a.A[1] = dG; a.lda = s.ldi; a.a_lay = act_k(s); a.a_bytes = act_ext;
+    a.B[0] = u; a.B[1] = g; a.ldb = s.f8; a.b_lay = s.bf16 ? LAY_KC2 : LAY_KC; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
     a.segs = s.planes;
     a.C[0] = dX; a.ldc = s.d;
     if (launch_plain(a, EPI_OUT, s.bf16, part, st)) return -1;
@@ -134,8 +142,8 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   if (dW1 || dWg) {
     // dW1 = X^T dU, dWg = X^T dG: one launch if both are wanted
     a = product(s.d, s.f, s.T);
-    a.A[0] = X; a.lda = s.d; a.a_mc = 1; a.a_bytes = x_ext;
-    a.B[0] = dW1 ? dU : dG; a.B[1] = dG; a.ldb = s.ldi; a.b_mc = 1; a.b_bytes = act_ext;
+    a.A[0] = X; a.lda = s.d; a.a_lay = LAY_MC; a.a_bytes = x_ext;
+    a.B[0] = dW1 ? dU : dG; a.B[1] = dG; a.ldb = s.ldi; a.b_lay = act_m(s); a.b_bytes = act_ext;
     a.C[0] = dW1 ? dW1 : dWg; a.C[1] = dWg; a.ldc = s.f;
     a.twin = dW1 && dWg;
     a.out_f32 = grad_f32; a.accumulate = accumulate;
@@ -144,8 +152,8 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   if (dW2) {
     // dW2 = H^T dY
     a = product(s.f, s.d, s.T);
-    a.A[0] = H; a.lda = s.ldi; a.a_mc = 1; a.a_bytes = act_ext;
-    a.B[0] = dY; a.ldb = s.d; a.b_mc = 1; a.b_bytes = x_ext;
+    a.A[0] = H; a.lda = s.ldi; a.a_lay = act_m(s); a.a_bytes = act_ext;
+    a.B[0] = dY; a.ldb = s.d; a.b_lay = LAY_MC; a.b_bytes = x_ext;
     a.C[0] = dW2; a.ldc = s.d;
     a.out_f32 = grad_f32; a.accumulate = accumulate;
     if (launch_plain(a, EPI_OUT, s.bf16, part, st)) return -1;
