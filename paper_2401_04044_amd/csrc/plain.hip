@@ -605,21 +605,21 @@ struct Plan { int shape, split; };
 
 // Choice of the tile and of the ranges that the reduction is cut into, by estimated time (us): t[k - 1] a slab with k
 // workgroups on a CU, per_cu of which a CU holds at a time, `fixed` for filling the ring and storing.  256 CUs; the
-// fullest one sets the time.  The figures are a least-squares fit to 3400 timings of 258 products (1 to 4096 rows, the
-// layers' widths from 256 to 5120) on every tile and up to 16 ranges; the chosen one takes 2 % (bf16) and 0.2 % (fp32)
-// longer than the best on average.
-struct ShapeCost { int bm, bn, per_cu; float t[4], fixed; };
-static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.246f, 0.452f}, 4.9f},
-                                                {256, 256, 1, {0.514f}, 7.0f},
-                                                {64, 64, 4, {0.138f, 0.227f, 0.497f, 0.546f}, 3.9f}};
-static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {1.05f, 1.61f}, 1.6f}, {}, {64, 64, 4, {0.348f, 0.570f, 0.989f, 1.21f}, 0.3f}};
+// fullest one sets the time.  The figures are a least-squares fit to 5400 timings of 460 products (1 to 6000 rows, the
+// layers' widths from 256 to 5120, operands that no cache holds) on every tile and up to 16 ranges; the chosen one
+// takes 1.5 % (bf16) and 0.5 % (fp32) longer than the best on average, 9 % and 3 % in the 95th percentile.
+struct ShapeCost { int bm, bn, per_cu; float t[3], fixed; };
+static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.236f, 0.447f}, 4.0f}, {256, 256, 1, {0.489f}, 6.1f},
+                                                {64, 64, 3, {0.131f, 0.263f, 0.398f}, 3.4f}};
+static const ShapeCost SHAPE_BF16_GATED64 = {64, 128, 2, {0.204f, 0.423f}, 3.5f};
+static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {0.972f, 1.458f}, 1.7f}, {}, {64, 64, 3, {0.318f, 0.576f, 0.898f}, 0.5f}};
 struct ProductCost {
-  float layout[3];        // factor of a slab: right operand mc, both kc, both mc
+  float layout[3];        // factor of a slab: right operand turned round, neither, both
   float bw, overlap;      // bytes a us, and the share of the traffic's time that comes on top
   float sum, sum_range, sum_bw;   // adding ranges: a launch, each range, bytes a us
 };
-static const ProductCost COST_BF16 = {{1.0f, 1.08f, 1.17f}, 4.55e6f, 0.2f, 1.0f, 0.3f, 2.65e6f};
-static const ProductCost COST_F32 = {{1.0f, 0.98f, 1.06f}, 2.04e6f, 0.22f, 1.6f, 0.26f, 1.91e6f};
+static const ProductCost COST_BF16 = {{1.0f, 1.12f, 1.26f}, 4.82e6f, 0.34f, 1.56f, 0.13f, 2.30e6f};
+static const ProductCost COST_F32 = {{1.0f, 1.01f, 1.05f}, 2.17e6f, 0.29f, 2.0f, 0.085f, 1.61e6f};
 constexpr size_t PART_ROOM = (size_t)32 << 20;   // scratch for ranges' sums
 
 static inline bool turned(int lay) { return lay == LAY_MC || lay == LAY_BM; }
@@ -635,13 +635,13 @@ static Plan plain_plan(const PlainArgs& a, int epi, int bf16) {
   Plan best = {PS_128x128, 1};
   float best_t = 1e30f;
   for (int s = 0; s < PS_SHAPES; ++s) {
-    const ShapeCost& q = bf16 ? SHAPE_BF16[s] : SHAPE_F32[s];
+    const ShapeCost& q = !bf16 ? SHAPE_F32[s] : s == PS_64x64 && epi == EPI_GLU ? SHAPE_BF16_GATED64 : SHAPE_BF16[s];
     if (q.bm == 0) continue;
-    const int bn = epi == EPI_GLU && !(bf16 && s == PS_64x64) ? q.bn / 2 : q.bn;
+    const int bn = epi == EPI_GLU ? q.bn / 2 : q.bn;
     const int64_t tiles = (int64_t)((a.M + q.bm - 1) / q.bm) * ((a.n_store + bn - 1) / bn) * (a.twin ? 2 : 1);
     for (int split = 1; split <= 16; split += split < 4 ? 1 : split < 8 ? 2 : 4) {
       const size_t part = (size_t)split * planes * a.M * a.n_store * 4;
-      if (split > 1 && (part > PART_ROOM || tiles * split > 768 || slabs / split < 4)) break;
+      if (split > 1 && (part > PART_ROOM || tiles * split > 1024 || slabs / split < 4)) break;
       const int n = (slabs + split - 1) / split;
       const int64_t load = (tiles * split + 255) / 256, full = load / q.per_cu, rest = load % q.per_cu;
       float t = (float)full * (n * q.t[q.per_cu - 1] * layout + q.fixed);
