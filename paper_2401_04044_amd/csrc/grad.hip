@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const Group g, const flo
       for (int q = 0; q < CHUNK / 4096; ++q) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[q][e] = scale(v[q][e]);
-        *(u32x4_t*)(dst + (q * 256 + threadIdx.x) * 16) = v[q];
+        __builtin_nontemporal_store(v[q], (u32x4_t*)(dst + (q * 256 + threadIdx.x) * 16));
       }
     } else {
       const int whole = left & ~15;

@@ -557,17 +557,19 @@ __global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
   emit8<T, EPI>(p, which, row, col, v, u);
 }
 
-// blockIdx.y: which of the two matrices
+// A workgroup per row, eight elements a thread; blockIdx.y: which of the two matrices.
 template <typename T>
-__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* src1, T* dst0, T* dst1, int64_t rows, int cols,
-                                                       int cols8) {
-  const T* const src = blockIdx.y ? src1 : src0;
-  T* const dst = blockIdx.y ? dst1 : dst0;
-  const int64_t n = rows * cols8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / cols8;
-    const int c = (int)(i % cols8);
-    dst[i] = c < cols ? src[r * cols + c] : (T)0;
+__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* src1, T* dst0, T* dst1, int cols, int cpr) {
+  const T* const src = (blockIdx.y ? src1 : src0) + (int64_t)blockIdx.x * cols;
+  T* const dst = (blockIdx.y ? dst1 : dst0) + (int64_t)blockIdx.x * cpr * 8;
+  for (int i = threadIdx.x; i < cpr; i += blockDim.x) {
+    T v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i * 8 + e < cols ? src[i * 8 + e] : (T)0;
+    u32x4_t w[sizeof(T) / 2];
+    __builtin_memcpy(w, v, sizeof(v));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) ((u32x4_t*)(dst + i * 8))[k] = w[k];
   }
 }
 
@@ -715,15 +717,14 @@ int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st) {
   return bf16 ? launch_typed<uint16_t>(a, epi, pl.shape, st) : launch_typed<float>(a, epi, pl.shape, st);
 }
 
-int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int64_t rows, int cols, int bf16, hipStream_t st) {
-  const int cols8 = (cols + 7) / 8 * 8;
-  const int64_t n = rows * cols8;
-  if (n <= 0) return 0;
-  const dim3 grid((unsigned)std::min<int64_t>((n + 1023) / 1024, 2048), src1 ? 2 : 1);
-  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t*)src0, (const uint16_t*)src1,
-                               (uint16_t*)dst0, (uint16_t*)dst1, rows, cols, cols8);
-  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, dim3(256), 0, st, (const uint32_t*)src0, (const uint32_t*)src1,
-                          (uint32_t*)dst0, (uint32_t*)dst1, rows, cols, cols8);
+int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int rows, int cols, int bf16, hipStream_t st) {
+  if (rows <= 0 || cols <= 0) return 0;
+  const int cpr = (cols + 7) / 8;
+  const dim3 grid(rows, src1 ? 2 : 1), block(cpr > 128 ? 256 : 64);
+  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, block, 0, st, (const uint16_t*)src0, (const uint16_t*)src1,
+                               (uint16_t*)dst0, (uint16_t*)dst1, cols, cpr);
+  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, block, 0, st, (const uint32_t*)src0, (const uint32_t*)src1,
+                          (uint32_t*)dst0, (uint32_t*)dst1, cols, cpr);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
