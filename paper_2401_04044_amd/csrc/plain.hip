@@ -557,6 +557,89 @@ __global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
   emit8<T, EPI>(p, which, row, col, v, u);
 }
 
+// The weights' gradients of at most 32 tokens: a reduction of one slab, so that the output's traffic is all there is.
+// The kernel above then spends its time on starting workgroups (a wavefront takes an XCD 24 clocks to start) and on
+// one dependent round trip each.  Here three workgroups a CU walk over the 128x128 tiles and fetch the next one's
+// operands before they multiply and store the present one.
+// (Both operands turned round, bf16.)
+template <int LA_, int LB_>
+__global__ void __launch_bounds__(256) outer_kernel(const PlainArgs p, int tiles_m, int tiles_n1, int tiles) {
+  using SA = Side<uint16_t, 128, LA_>;
+  using SB = Side<uint16_t, 128, LB_>;
+  constexpr int BUF = 16 * 1024, PITCH = 64 * 4 + 16;   // a slab of both operands; staging of 16 rows a wavefront
+  __shared__ __attribute__((aligned(16))) char smem[2 * BUF + 4 * 16 * PITCH];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const uint32_t lds0 = lds_offset(smem);
+  int k = 0;
+  uint32_t va[2], vb[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    va[i] = SA::source(wave + i * 4, lane, (uint32_t)p.lda, &k);
+    vb[i] = SB::source(wave + i * 4, lane, (uint32_t)p.ldb, &k);
+  }
+  struct Where { int m0, n0, which; };
+  auto where = [&](int t) {
+    const int tn2 = t / tiles_m, which = tn2 >= tiles_n1;
+    return Where{(t - tn2 * tiles_m) * 128, (which ? tn2 - tiles_n1 : tn2) * 128, which};
+  };
+  auto fetch = [&](const Where& w, int buf) {
+    const int64_t ao = SA::origin(w.m0, p.lda), bo = SB::origin(w.n0, p.ldb);
+    const u32x4_t ra = resource((const char*)p.A[0] + ao, p.a_bytes - ao);
+    const u32x4_t rb = resource((const char*)(w.which ? p.B[1] : p.B[0]) + bo, p.b_bytes - bo);
+    const uint32_t st = lds0 + buf * BUF + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      load_to_lds(ra, st + i * 4096, va[i], 0);
+      load_to_lds(rb, st + 8192 + i * 4096, vb[i], 0);
+    }
+  };
+  const uint32_t la = lds0 + SA::first(wm * 4, lane), lb = lds0 + 8192 + SB::first(wn * 4, lane);
+  char* const own = smem + 2 * BUF + wave * (16 * PITCH);
+  int t = blockIdx.x, buf = 0;
+  if (t >= tiles) return;
+  Where w = where(t);
+  fetch(w, 0);
+  while (true) {
+    wait_vmcnt<0>();
+    wait_lgkmcnt<0>();
+    lds_barrier();   // this tile's operands are there for all; all are done with the other buffer
+    const int tn = t + gridDim.x;
+    const Where next = where(tn < tiles ? tn : t);
+    if (tn < tiles) fetch(next, buf ^ 1);
+    Frag fa[4], fb[4];
+    f32x4_t acc[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) SB::read(fb[j], lb + buf * BUF, j, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) SA::read(fa[i], la + buf * BUF, i, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j].v, fa[i].v, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    const int col = w.n0 + wn * 64 + (lane & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *(f32x4_t*)(own + (lane & 15) * PITCH + (j * 16 + 4 * (lane >> 4)) * 4) = acc[i][j];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int r = q * 8 + (lane >> 3);
+        float v[8], u[8];
+        load8<float>(own + r * PITCH + (lane & 7) * 32, 0, v);
+        const int64_t row = w.m0 + wm * 64 + i * 16 + r;
+        if (row < p.M && col < p.n_store) emit8<uint16_t, EPI_OUT>(p, w.which, row, col, v, u);
+      }
+    }
+    if (tn >= tiles) break;
+    t = tn;
+    w = next;
+    buf ^= 1;
+  }
+}
+
 // A workgroup per row, eight elements a thread; blockIdx.y: which of the two matrices.
 template <typename T>
 __global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* src1, T* dst0, T* dst1, int cols, int cpr) {
@@ -685,6 +768,15 @@ static int launch_whole(const PlainArgs& a, int shape, hipStream_t st) {
   return rc == 0 && a.part ? launch_reduce<T, EPI>(a, st) : rc;
 }
 
+template <int LA_, int LB_>
+static int launch_outer(const PlainArgs& a, hipStream_t st) {
+  const int64_t tiles_m = (a.M + 127) / 128, tiles_n1 = (a.n_store + 127) / 128, tiles = tiles_m * tiles_n1 * (a.twin ? 2 : 1);
+  if (tiles > 0x3fffffff) return -1;
+  hipLaunchKernelGGL((outer_kernel<LA_, LB_>), dim3((unsigned)std::min<int64_t>(tiles, 3 * 256)), dim3(256), 0, st, a, (int)tiles_m,
+                     (int)tiles_n1, (int)tiles);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
 // The products of the two passes and the way their operands lie.
 template <typename T>
 static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) {
@@ -697,6 +789,8 @@ static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) 
     case EPI_OUT:
       if (!turned(a.a_lay) && turned(a.b_lay)) return launch_whole<T, ACT_K, LAY_MC, EPI_OUT>(a, shape, st);        // H W2
       if (!turned(a.a_lay)) return launch_whole<T, ACT_K, BF ? LAY_KC2 : LAY_KC, EPI_OUT>(a, shape, st);            // dU W1^T
+      if constexpr (BF)
+        if (a.K <= 32 && !a.part) return a.a_lay == LAY_MC ? launch_outer<LAY_MC, LAY_BM>(a, st) : launch_outer<LAY_BM, LAY_MC>(a, st);
       if (a.a_lay == LAY_MC) return launch_whole<T, LAY_MC, ACT_M, EPI_OUT>(a, shape, st);                          // X^T dU
       return launch_whole<T, ACT_M, LAY_MC, EPI_OUT>(a, shape, st);                                                 // H^T dY
   }
