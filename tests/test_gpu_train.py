@@ -59,7 +59,7 @@ def _check_layer(ff, T, d, f, gated, dtype, seed=0, **kw):
 
 # one token, a few, tile edges and beyond; widths below a tile, odd, aligned, more than one tile; reductions
 # shorter than a slab and with remainders
-SHAPES = [(1, 8, 1), (1, 264, 1000), (2, 64, 7), (3, 136, 130), (16, 64, 64), (17, 72, 129), (33, 520, 96), (64, 128, 256),
+SHAPES = [(1, 8, 1), (32, 200, 300), (31, 136, 2050), (1, 264, 1000), (2, 64, 7), (3, 136, 130), (16, 64, 64), (17, 72, 129), (33, 520, 96), (64, 128, 256),
           (65, 256, 550), (129, 136, 257), (200, 264, 1003), (300, 512, 640)]
 
 
@@ -75,9 +75,10 @@ def test_layer_with_large_tiles(ff, T, d, f, gated):
     _check_layer(ff, T, d, f, gated, "bf16")
 
 
+@pytest.mark.parametrize("T", [20, 70])           # (up to 32 tokens the bf16 gradients have a kernel of their own)
 @pytest.mark.parametrize("dtype,f", [("bf16", 96), ("bf16", 99), ("f32", 99)])
-def test_gradients_in_fp32_and_accumulated(ff, dtype, f):
-    T, d = 70, 64
+def test_gradients_in_fp32_and_accumulated(ff, dtype, f, T):
+    d = 64
     _check_layer(ff, T, d, f, True, dtype, grad_f32=True)
     rng = np.random.default_rng(8)
     host = tu.make_layer(rng, d, f, True, T, dtype)
@@ -149,6 +150,20 @@ def test_a_bad_token_stays_alone(ff, T):
         assert not torch.isfinite(gb["W2"]).all()
 
 
+def test_a_factor_beyond_fp16_is_not_hidden(ff):
+    """A kept derivative beyond 65504 makes the gradients behind it non-finite; one below it does not."""
+    T, d, f = 4, 64, 40
+    host = tu.make_layer(np.random.default_rng(14), d, f, True, T, "bf16")
+    desc = ff.make_desc(d, f, "swiglu", "bf16")
+    X, W1, Wg, W2, dY = tu.to_dev(host, "bf16")
+    for scale, fine in ((512.0, True), (1e7, False)):     # |z| of some tens, of some hundred thousand
+        Y, kept = ff.dense_forward(desc, X * scale, W1, Wg, W2, want_saved=True)
+        assert torch.isfinite(Y).all()
+        dX, g = ff.dense_backward(desc, X * scale, W1, Wg, W2, kept, dY)
+        _, flag = ff.grad_norm([g["W1"], g["Wg"]])
+        assert (int(flag) == 0) == fine and bool(torch.isfinite(dX).all()) == fine
+
+
 def test_memory_around_the_operands_is_not_used(ff):
     """Rows behind the last and in front of the first are NaN: nothing of them reaches a result, nothing is written there."""
     T, d, f = 37, 72, 101
@@ -175,6 +190,64 @@ def test_memory_around_the_operands_is_not_used(ff):
             assert torch.equal(got, ref)
         for buf in list(bufs) + [o[0] for o in outs]:
             assert torch.isnan(buf[:pad]).all() and torch.isnan(buf[-pad:]).all()
+
+
+@pytest.mark.parametrize("T,d,f", [(1, 72, 99), (31, 200, 1500), (32, 1000, 300), (33, 264, 131), (47, 72, 2050), (100, 136, 37)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_buffers_may_hold_anything(ff, T, d, f, dtype):
+    """Scratch and kept state full of NaN patterns before the call: the same bits as with zeros."""
+    host = tu.make_layer(np.random.default_rng(T), d, f, True, T, dtype)
+    desc = ff.make_desc(d, f, "swiglu", dtype)
+    X, W1, Wg, W2, dY = tu.to_dev(host, dtype)
+
+    def go(byte):
+        kept = torch.full((ff.dense_kept_bytes(desc, T),), byte, dtype=torch.uint8, device="cuda")
+        w1 = torch.full((ff.workspace_bytes(desc, ff.WS_DENSE_FORWARD, T),), byte, dtype=torch.uint8, device="cuda")
+        w2 = torch.full((ff.workspace_bytes(desc, ff.WS_DENSE_BACKWARD, T),), byte, dtype=torch.uint8, device="cuda")
+        alone = ff.dense_forward(desc, X, W1, Wg, W2, workspace=w1)
+        w1.fill_(byte)
+        Y = ff.dense_forward(desc, X, W1, Wg, W2, saved=kept, workspace=w1)[0]
+        dX, g = ff.dense_backward(desc, X, W1, Wg, W2, kept, dY, workspace=w2)
+        return [alone, Y, dX, g["W1"], g["Wg"], g["W2"]]
+
+    for a, b in zip(go(0), go(0xFF)):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_weights_beyond_two_gib(ff, T):
+    """Offsets into the weights pass 32 bits, along either axis of them."""
+    d, f = 8192, 139_264
+    assert d * f * 2 > 1 << 31
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+
+    def normal(shape, std):
+        out = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+        for part in out.split(max(1, (1 << 27) // shape[1])):
+            part.copy_(torch.randn(part.shape, generator=g, device="cuda").mul_(std))
+        return out
+
+    W1, W2 = normal((d, f), 0.01), normal((f, d), 0.01)
+    X, dY = normal((T, d), 1.0), normal((T, d), 1.0)
+    desc = ff.make_desc(d, f, "gelu", "bf16")
+    Y, kept = ff.dense_forward(desc, X, W1, None, W2, want_saved=True)
+    dX, dW = ff.dense_backward(desc, X, W1, None, W2, kept, dY)
+    want_Y, want_dX = torch.zeros(T, d, device="cuda"), torch.zeros(T, d, device="cuda")
+    x, dy, step = X.float(), dY.float(), 8704
+    for a in range(0, f, step):
+        w1, w2 = W1[:, a:a + step].float(), W2[a:a + step].float()
+        z = (x @ w1).double()
+        cdf = 0.5 * torch.erfc(-z / math.sqrt(2.0))
+        H, D = (z * cdf).float(), (cdf + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)).float()
+        want_Y += H @ w2
+        dU = (dy @ w2.t()) * D
+        want_dX += dU @ w1.t()
+        if a in (0, f - step):
+            for got, ref in ((dW["W1"][:, a:a + step], x.t() @ dU), (dW["W2"][a:a + step], H.t() @ dy)):
+                assert float((got.float() - ref).norm() / ref.norm()) < gu.TOL["bf16"]
+    for got, ref in ((Y, want_Y), (dX, want_dX)):
+        assert float((got.float() - ref).norm() / ref.norm()) < gu.TOL["bf16"]
 
 
 def test_no_tokens(ff):

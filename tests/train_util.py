@@ -1,7 +1,8 @@
 """How far the training path may be from exact arithmetic, entry by entry, and helpers for its tests.
 
-The library rounds H, the kept derivatives D (dH/dz, dH/du), dU, dG and its outputs to the storage type, each
-by at most u times the value (u: bf16 2^-8, fp32 2^-24), and forms every sum of n products in fp32: off by at
+The library rounds H, dU, dG and its outputs to the storage type, each by at most u times the value (u: bf16 2^-8,
+fp32 2^-24), and the kept derivatives D (dH/dz, dH/du) to fp16 in bf16 layers (at most 2^-11 of the value, and 2^-25
+where it is below fp16's normal range), to fp32 in fp32 layers; it forms every sum of n products in fp32: off by at
 most g(n) = n 2^-23 times the sum of magnitudes, whatever the order.  Pre-activations are therefore off by
 e = g(d) |X| |W|.  With |silu'| <= 1.1, |silu''| <= 0.5, |gelu'| <= 1.13, |gelu''| <= 0.8 and activations
 whose sigmoid or normal distribution is off by at most a = 1e-6:
@@ -13,6 +14,7 @@ import numpy as np
 import gpu_util as gu
 
 U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+UD = {2.0 ** -8: (2.0 ** -11, 2.0 ** -25), 2.0 ** -24: (2.0 ** -24, 0.0)}     # of the kept derivatives, by u
 A = 1e-6
 
 
@@ -32,16 +34,17 @@ def dense_bounds(X, W1, Wg, W2, kept, dY, u, u_grad):
     z, H, dz, dH = abs(z), abs(H), abs(dz), abs(dH)
     T, d = X.shape
     f = H.shape[1]
+    ud, ad = UD[u]
     if Wg is None:
         e = g(d) * (X @ W1)
         eH = 1.13 * e + A * z + u * H
-        D = [(dz, 0.8 * e + A * (1 + z) + u * dz, W1, "W1")]
+        D = [(dz, 0.8 * e + A * (1 + z) + ud * dz + ad, W1, "W1")]
     else:
         Wg, up, du = _f8(Wg), abs(up), abs(du)
         ez, eu = g(d) * (X @ Wg), g(d) * (X @ W1)
         silu = 1.1 * ez + A * z
         eH = silu * (up + eu) + du * eu + u * H
-        D = [(du, silu + u * du, W1, "W1"), (dz, (0.5 * ez + A * (1 + z)) * (up + eu) + 1.1 * eu + u * dz, Wg, "Wg")]
+        D = [(du, silu + ud * du + ad, W1, "W1"), (dz, (0.5 * ez + A * (1 + z)) * (up + eu) + 1.1 * eu + ud * dz + ad, Wg, "Wg")]
     M = dY @ W2.T                                   # dH is off by g(d) M
     out = {"Y": eH @ W2 + g(f) * ((H + eH) @ W2)}
     out["W2"] = eH.T @ dY + g(T) * ((H + eH).T @ dY)
