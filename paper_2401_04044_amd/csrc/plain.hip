@@ -685,27 +685,29 @@ static int launch_tile(const PlainArgs& a, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_SHAPES = 3 };
+enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_256x128 = 3, PS_SHAPES = 4 };
 struct Plan { int shape, split; };
 
 // Choice of the tile and of the ranges that the reduction is cut into, by estimated time (us): t[k - 1] a slab with k
 // workgroups on a CU, per_cu of which a CU holds at a time, `fixed` for filling the ring and storing.  256 CUs; the
-// fullest one sets the time.  The figures are a least-squares fit to 5400 timings of 460 products (1 to 6000 rows, the
+// fullest one sets the time.  The figures are a least-squares fit to 6800 timings of 460 products (1 to 6000 rows, the
 // layers' widths from 256 to 5120, operands that no cache holds) on every tile and up to 16 ranges; the chosen one
-// takes 1.5 % (bf16) and 0.5 % (fp32) longer than the best on average, 9 % and 3 % in the 95th percentile.
+// takes 1.2 % (bf16) and 0.3 % (fp32) longer than the best on average, 8 % and 2 % in the 95th percentile.  What they
+// show: an XCD's L2 hands its 32 CUs 64 bytes per channel and clock, 64 KB a us and CU, so that two 128x128 tiles (32 KB
+// a slab) take as long as their MFMAs would twice over, and one 256x256 tile as long as its own.
 struct ShapeCost { int bm, bn, per_cu; float t[3], fixed; };
-static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.236f, 0.447f}, 4.0f}, {256, 256, 1, {0.489f}, 6.1f},
-                                                {64, 64, 3, {0.131f, 0.263f, 0.398f}, 3.4f}};
-static const ShapeCost SHAPE_BF16_GATED64 = {64, 128, 2, {0.204f, 0.423f}, 3.5f};
-static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {0.972f, 1.458f}, 1.7f}, {}, {64, 64, 3, {0.318f, 0.576f, 0.898f}, 0.5f}};
+static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.252f, 0.477f}, 2.5f}, {256, 256, 1, {0.547f}, 4.2f},
+                                                {64, 64, 3, {0.144f, 0.276f, 0.449f}, 1.8f}, {256, 128, 1, {0.355f}, 3.0f}};
+static const ShapeCost SHAPE_BF16_GATED64 = {64, 128, 2, {0.203f, 0.433f}, 2.1f};
+static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {0.992f, 1.607f}, 1.7f}, {}, {64, 64, 3, {0.324f, 0.588f, 0.919f}, 0.5f}, {}};
 struct ProductCost {
   float layout[3];        // factor of a slab: right operand turned round, neither, both
   float bw, overlap;      // bytes a us, and the share of the traffic's time that comes on top
   float sum, sum_range, sum_bw;   // adding ranges: a launch, each range, bytes a us
 };
-static const ProductCost COST_BF16 = {{1.0f, 1.12f, 1.26f}, 4.82e6f, 0.34f, 1.56f, 0.13f, 2.30e6f};
-static const ProductCost COST_F32 = {{1.0f, 1.01f, 1.05f}, 2.17e6f, 0.29f, 2.0f, 0.085f, 1.61e6f};
-constexpr size_t PART_ROOM = (size_t)32 << 20;   // scratch for ranges' sums
+static const ProductCost COST_BF16 = {{1.0f, 1.07f, 1.11f}, 4.91e6f, 0.34f, 1.7f, 0.12f, 2.29e6f};
+static const ProductCost COST_F32 = {{1.0f, 0.99f, 0.99f}, 2.20e6f, 0.22f, 2.0f, 0.10f, 1.70e6f};
+constexpr size_t PART_ROOM = (size_t)64 << 20;   // scratch for ranges' sums
 
 static inline bool turned(int lay) { return lay == LAY_MC || lay == LAY_BM; }
 
@@ -751,6 +753,7 @@ static int launch_shape(const PlainArgs& a, int shape, hipStream_t st) {
   }
   if constexpr (BF) {
     if (shape == PS_256x256) return launch_tile<T, 256, 256, 2, 4, 4, LA_, LB_, EPI>(a, st);
+    if (shape == PS_256x128) return launch_tile<T, 256, 128, 4, 2, 4, LA_, LB_, EPI>(a, st);
   }
   return -1;
 }
