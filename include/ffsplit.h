@@ -308,8 +308,8 @@ int ffsplit_stack_forward(const ffsplit_desc_t* desc, int32_t n_layers, const vo
  * row-major): an optimiser changes them every step, so nothing is packed.  The heavy part FFN_1 of a
  * split is such a layer of k neurons (columns h2 of W1 and Wg, rows h2 of W2).
  * Of the descriptor they read d_model (a multiple of 8), d_ff (any number), act and dtype; k, rem_kind,
- * rank and group are ignored.  d_model and d_ff are below 2^20.  No buffer that a call writes may
- * overlap another one of the call, but where it is said.
+ * rank and group are ignored.  d_model is at most 2^20, d_ff 2^20 - 64 and T 2^28.  No buffer that a call
+ * writes may overlap another one of the call, but where it is said.
  */
 
 /* Bytes of what ffsplit_dense_forward keeps for the backward pass (pure host arithmetic, never less for
@@ -360,7 +360,7 @@ int ffsplit_dense_backward(const ffsplit_desc_t* desc, const void* X, int64_t T,
  *   dx = [residual +] r dn - x r^3 mean(x * dn).
  * x, dx, residual fp32 [T, d_model]; residual (NULL: none) is the gradient that goes around the norm, and
  * may be the same buffer as dx.  dx_cast: NULL, or [T, d_model] in `dtype`, receives dx as well (the
- * gradient that the layer below takes).  All arithmetic in fp32.
+ * gradient that the layer below takes).  All arithmetic in fp32.  d_model is at most 2^20.
  */
 int ffsplit_token_rmsnorm_backward(const float* x, const void* dn, int64_t T, int32_t d_model, float eps,
                                    int32_t dtype, const float* residual, float* dx, void* dx_cast, void* stream);
@@ -378,7 +378,8 @@ int ffsplit_grad_norm(int32_t n, const void* const* grads, const int64_t* counts
 /*
  * Clipping by that norm: out[i] = grads[i] * (max_norm / *norm) where *norm > max_norm; otherwise, and
  * where *norm is not finite (the caller's program then skips the step), out[i] = grads[i] unchanged.
- * out: HOST array of n device pointers in the types of grads; out[i] == grads[i] scales in place.
+ * out: HOST array of n device pointers in the types of grads; out[i] == grads[i] scales in place.  (A tensor
+ * listed twice would be scaled twice.)
  * The norm is read on the device: nothing waits.  max_norm > 0 (infinity: nothing is scaled).
  */
 int ffsplit_grad_clip(int32_t n, const void* const* grads, const int64_t* counts, const int32_t* dtypes,

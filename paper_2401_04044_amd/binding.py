@@ -418,6 +418,8 @@ def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=
     if dX is None and want_dx:
         dX = torch.empty((T, desc.d_model), dtype=dt, device=dev)
     _take(dX, "dX", (T, desc.d_model), dt, dev)
+    if dX is not None and T and dX.data_ptr() in (dY.data_ptr(), X.data_ptr()):
+        raise ValueError("dX: the buffer of dY or X, which the weights' gradients read behind it")
     g = _grads_for(desc, grads, accumulate, grad_f32, dev)
     with _on(dev):
         ws = _scratch(workspace_bytes(desc, WS_DENSE_BACKWARD, T), workspace, dev)
@@ -470,6 +472,7 @@ class _GradList:
 
     def out_ptrs(self, grads, out):
         if out is None:
+            self._apart(self.ptrs)
             return self.ptrs
         if len(out) != self.n:
             raise ValueError(f"out: {len(out)} tensors for {self.n} gradients")
@@ -478,7 +481,13 @@ class _GradList:
             if o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous() or o.device != self.device:
                 raise ValueError("out: tensors like the gradients are wanted, contiguous and on their device")
             ptrs.append(o.data_ptr())
+        self._apart(ptrs)
         return (ctypes.c_void_p * max(self.n, 1))(*ptrs)
+
+    def _apart(self, ptrs):
+        written = [p for p, c in zip(ptrs, self.counts) if c]
+        if len(set(written)) != len(written):
+            raise ValueError("gradients: a tensor that is written is listed twice")
 
     def norm(self, norm, flag, workspace):
         dev = self.device
@@ -563,6 +572,9 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
         raise ValueError(f"gradients of {len(grads)} layers for {n}")
     g = [_grads_for(desc, grads[l] if grads is not None else None, accumulate, grad_f32, dev, f" of layer {l}")
          for l in range(n)]
+    written = [t.data_ptr() for q in g for t in q.values() if t is not None]
+    if len(set(written)) != len(written):
+        raise ValueError("gradients: a buffer is listed twice")
     W1, Wg, W2 = _stack_args(desc, layers, dev)
     gated = desc.act == ACT_SWIGLU
     with _on(dev):

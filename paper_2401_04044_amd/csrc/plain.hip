@@ -675,7 +675,7 @@ static int launch_tile(const PlainArgs& a, hipStream_t st) {
   const int bnh = EPI == EPI_GLU ? BN / 2 : BN;
   const int tiles_m = (a.M + BM - 1) / BM;
   const int64_t tiles = (int64_t)tiles_m * ((a.n_store + bnh - 1) / bnh) * (a.twin ? 2 : 1);
-  if (tiles > 0x7fffffff) return -1;
+  if (tiles * (WGM * WGN * 64) > 0xffffffffll) return -1;   // threads of a launch
   PlainArgs g = a;
   // as many row tiles per group as make an XCD's tiles read the fewest rows of both operands
   const int per_cu = lds <= 80 * 1024 ? 2 : 1;

@@ -20,14 +20,17 @@ inline bool misaligned256(const void* p) { return ((uintptr_t)p & 255u) != 0; }
     if ((expr) != 0) return FFSPLIT_E_HIP; \
   } while (0)
 
-// (1 << 20: a lane's byte offset inside a tile of a product fits 31 bits)
+// (widths: a lane's byte offset inside a tile of a product fits 31 bits; tokens: counts of rows, rounded up to
+// a tile's, and of workgroups fit theirs)
+constexpr int MAX_WIDTH = 1 << 20;
+constexpr int64_t MAX_TOKENS = (int64_t)1 << 28;
 int check_dense(const ffsplit_desc_t* d, int64_t T) {
   if (!d) return FFSPLIT_E_NULLPTR;
   if (d->d_model <= 0 || d->d_ff <= 0) return FFSPLIT_E_BADDESC;
   if (d->act != FFSPLIT_ACT_GELU && d->act != FFSPLIT_ACT_SWIGLU) return FFSPLIT_E_BADDESC;
   if (d->dtype != FFSPLIT_F32 && d->dtype != FFSPLIT_BF16) return FFSPLIT_E_BADDESC;
-  if (d->d_model % 8 != 0 || T < 0 || T > 0x7fffffff) return FFSPLIT_E_BADSHAPE;
-  if (d->d_model > (1 << 20) || d->d_ff > (1 << 20) - 64) return FFSPLIT_E_BADSHAPE;
+  if (d->d_model % 8 != 0 || T < 0 || T > MAX_TOKENS) return FFSPLIT_E_BADSHAPE;
+  if (d->d_model > MAX_WIDTH || d->d_ff > MAX_WIDTH - 64) return FFSPLIT_E_BADSHAPE;
   return FFSPLIT_OK;
 }
 
@@ -245,7 +248,7 @@ int ffsplit_dense_backward(const ffsplit_desc_t* d, const void* X, int64_t T, co
 
 int ffsplit_token_rmsnorm_backward(const float* x, const void* dn, int64_t T, int32_t d_model, float eps, int32_t dtype,
                                    const float* residual, float* dx, void* dx_cast, void* stream) {
-  if (d_model <= 0 || d_model % 8 != 0 || T < 0 || T > 0x7fffffff) return FFSPLIT_E_BADSHAPE;
+  if (d_model <= 0 || d_model % 8 != 0 || d_model > MAX_WIDTH || T < 0 || T > 0x7fffffff) return FFSPLIT_E_BADSHAPE;
   if (dtype != FFSPLIT_F32 && dtype != FFSPLIT_BF16) return FFSPLIT_E_BADDESC;
   if (T == 0) return FFSPLIT_OK;
   if (!x || !dn || !dx) return FFSPLIT_E_NULLPTR;

@@ -221,3 +221,37 @@ def test_binding_refuses_views_types_and_shapes():
         ff.grad_clip([X, X], torch.zeros(1), 1.0, out=[X])
     with pytest.raises(TypeError):
         ff.token_rmsnorm_backward(X, X.half())
+
+
+def test_the_largest_sizes_are_refused_and_not_wrapped():
+    """Rows beyond 2^28 and widths beyond 2^20: counts of them, rounded up, would pass 31 bits."""
+    import paper_2401_04044_amd as ff
+    L, ref = ff.lib, ctypes.byref
+    for desc in (ff.make_desc(8, 8, "gelu", "bf16"), ff.make_desc(8, 8, "swiglu", "f32")):
+        for T in ((1 << 28) + 1, (1 << 31) - 16, (1 << 31) - 1):
+            assert _forward(L, ref(desc), T=T) == -3 and _backward(L, ref(desc), T=T) == -3
+            assert ff.dense_kept_bytes(desc, T) == 0 and ff.workspace_bytes(desc, ff.WS_DENSE_FORWARD, T) == 0
+        assert ff.dense_kept_bytes(desc, 1 << 28) >= (2 if desc.act == ff.ACT_GELU else 3) * 8 * (1 << 28) * (2 if desc.dtype == ff.BF16 else 4)
+    for d in ((1 << 20) + 8, (1 << 31) - 8):
+        assert L.ffsplit_token_rmsnorm_backward(FAKE, FAKE, 1, d, 1e-6, 1, None, FAKE, None, None) == -3
+
+
+def test_binding_refuses_buffers_used_twice():
+    import torch
+    import paper_2401_04044_amd as ff
+    d = ff.make_desc(64, 100, "gelu", "f32")
+    X, dY, W, V, one = torch.zeros(4, 64), torch.zeros(4, 64), torch.zeros(64, 100), torch.zeros(100, 64), torch.zeros(1)
+    saved = torch.zeros(1 << 20, dtype=torch.uint8)
+    for dX in (X, dY):
+        with pytest.raises(ValueError, match="dX"):
+            ff.dense_backward(d, X, W, None, V, saved, dY, dX=dX)
+    with pytest.raises(ValueError, match="twice"):
+        ff.grad_clip([X, W, X], one, 1.0)
+    with pytest.raises(ValueError, match="twice"):
+        ff.grad_clip([X, dY], one, 1.0, out=[X, X])
+    with pytest.raises(ValueError, match="twice"):
+        ff.clip_grad_norm([X, X], 1.0)
+    layers = [{"W1": W, "W2": V}, {"W1": W, "W2": V}]
+    grads = [{"W1": W, "W2": V}, {"W1": W, "W2": torch.zeros(100, 64)}]
+    with pytest.raises(ValueError, match="twice"):
+        ff.dense_stack_backward(d, layers, saved, X, grads=grads)
