@@ -270,8 +270,9 @@ int for_groups(const GradSet& set, F f) {
 int launch_rmsnorm_backward(const float* x, const void* dn, int64_t T, int d, float eps, int bf16, const float* residual,
                             float* dx, void* dx_cast, hipStream_t st) {
   if (T <= 0) return 0;
-  // a wavefront per row up to 2048 elements, a workgroup beyond
-  const bool wide = d > 2048;
+  // a wavefront per row up to 1024 elements, a workgroup beyond (us with a wavefront / a workgroup, bf16, 16384 rows of
+  // 512 22 / 35, 1024 40 / 45, 1536 64 / 63, 2048 99 / 91, 8192 500 / 390; 64 rows of 512 4.2 / 3.7, 8192 11 / 4.9)
+  const bool wide = d > 1024;
   const int64_t blocks = wide ? T : (T + 3) / 4;
   const dim3 grid((unsigned)std::min<int64_t>(blocks, 1 << 20));
 #define FFS_GO(B, N) hipLaunchKernelGGL((rmsnorm_backward_kernel<B, N>), grid, dim3(256), 0, st, x, dn, T, d, eps, residual, dx, dx_cast)

@@ -64,7 +64,8 @@ struct PlainArgs {
 size_t plain_part_room();
 // part: that many bytes
 int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st);
-// dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind, of one or two matrices; cols8 = cols rounded up to 8
+// dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind, of one or two matrices; cols8 = cols rounded up to 8; rows a
+// multiple of 8
 int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int rows, int cols, int bf16, hipStream_t st);
 
 }  // namespace ffsplit

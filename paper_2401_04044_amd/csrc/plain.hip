@@ -11,8 +11,8 @@
 //        0-3, 12-15, 20-27 and so on) then fall into different banks.
 //   KC2  the same fetched two slabs at a time, 128 bytes of a row: half the requests.  (64 bytes a row cost the
 //        memory pipeline up to a third of its rate: 4096 x 4096 x 22016 with both operands KC 614 us, with
-//        contiguous ones 460.)  A pair of slabs needs a third more LDS than its half of a ring of single ones, so
-//        that only one operand of a product can be fetched this way.
+//        contiguous ones 460, with one of them KC2 and the other contiguous 510.)  The ring needs one more pair, so that
+//        LDS has room for only one operand of a product fetched this way.
 //   MC   row-major, rows contiguous.  bf16 fragments are turned round on the way out of LDS (ds_read_b64_tr_b16:
 //        lane j of 16 gets column j of four 16-column rows), fp32 ones are read element by element.  Pieces of the
 //        LDS rows are exchanged by an XOR with the row number, so that the eight rows read at a time fall into
@@ -225,6 +225,10 @@ struct Walk {
   }
 };
 
+// Bound by the MFMAs (at the 1.8 to 1.95 GHz that these products run at) and by what the L2 hands out, which overlap all
+// but a fifth: 256x256 tiles, 4096 tokens, us a slab: 0.75; without loads 0.65, without LDS reads 0.59, without MFMAs 0.53.
+// At 4096 x 11008, 4096 tokens: X [Wg|W1] 600 us (1.23 PFLOP/s), H W2 259 (1.43), dY W2^T 354 (1.04), dU W1^T + dG Wg^T 509 (1.45),
+// X^T [dU|dG] 631 (1.17), H^T dY 315 (1.17).
 template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, int LA_, int LB_, int EPI>
 __global__ void __launch_bounds__(WGM* WGN * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 plain_kernel(const PlainArgs p) {
@@ -558,9 +562,9 @@ __global__ void __launch_bounds__(64) plain_reduce_kernel(const PlainArgs p) {
 }
 
 // The weights' gradients of at most 32 tokens: a reduction of one slab, so that the output's traffic is all there is.
-// The kernel above then spends its time on starting workgroups (a wavefront takes an XCD 24 clocks to start) and on
-// one dependent round trip each.  Here three workgroups a CU walk over the 128x128 tiles and fetch the next one's
-// operands before they multiply and store the present one.
+// The kernel above then spends its time on starting workgroups (180 of four wavefronts a us) and on one dependent
+// round trip each.  Here three workgroups a CU walk over the 128x128 tiles and fetch the next one's operands before
+// they multiply and store the present one.  4096 x 11008, 8 tokens: dW1 and dWg 65 -> 38 us (180 MB), dW2 39 -> 23.
 // (Both operands turned round, bf16.)
 template <int LA_, int LB_>
 __global__ void __launch_bounds__(256) outer_kernel(const PlainArgs p, int tiles_m, int tiles_n1, int tiles) {
@@ -640,19 +644,32 @@ __global__ void __launch_bounds__(256) outer_kernel(const PlainArgs p, int tiles
   }
 }
 
-// A workgroup per row, eight elements a thread; blockIdx.y: which of the two matrices.
-template <typename T>
-__global__ void __launch_bounds__(256) pad_rows_kernel(const T* src0, const T* src1, T* dst0, T* dst1, int cols, int cpr) {
-  const T* const src = (blockIdx.y ? src1 : src0) + (int64_t)blockIdx.x * cols;
-  T* const dst = (blockIdx.y ? dst1 : dst0) + (int64_t)blockIdx.x * cpr * 8;
-  for (int i = threadIdx.x; i < cpr; i += blockDim.x) {
-    T v[8];
+// A workgroup per row, in 32-bit words: neighbouring lanes on neighbouring ones, AT of a thread's under way.  (A row of
+// an odd number of bf16 begins in the middle of a word in every second row.  The matrix has a multiple of 8 rows, so
+// that each word with an element of it is whole.)  blockIdx.y: which of the two matrices.
+template <bool BF16>
+__global__ void __launch_bounds__(256) pad_rows_kernel(const uint32_t* src0, const uint32_t* src1, uint32_t* dst0, uint32_t* dst1,
+                                                       int cols, int words) {
+  constexpr int AT = 4, PER = BF16 ? 2 : 1;   // PER: elements of a word
+  const int64_t first = (int64_t)blockIdx.x * cols;
+  const uint32_t* const src = (blockIdx.y ? src1 : src0) + first / PER;
+  uint32_t* const dst = (blockIdx.y ? dst1 : dst0) + (int64_t)blockIdx.x * words;
+  const bool odd = BF16 && (first & 1);
+  for (int i0 = threadIdx.x; i0 < words; i0 += AT * 256) {
+    uint32_t v[AT], w[AT];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i * 8 + e < cols ? src[i * 8 + e] : (T)0;
-    u32x4_t w[sizeof(T) / 2];
-    __builtin_memcpy(w, v, sizeof(v));
+    for (int a = 0; a < AT; ++a) {
+      const int i = i0 + a * 256;
+      v[a] = i * PER < cols ? src[i] : 0u;
+      w[a] = odd && i * PER + 1 < cols ? src[i + 1] : 0u;
+    }
 #pragma unroll
-    for (int k = 0; k < (int)sizeof(T) / 2; ++k) ((u32x4_t*)(dst + i * 8))[k] = w[k];
+    for (int a = 0; a < AT; ++a) {
+      const int i = i0 + a * 256;
+      if (odd) v[a] = (v[a] >> 16) | (w[a] << 16);
+      else if (BF16 && i * PER + 1 >= cols) v[a] &= 0xffffu;
+      if (i < words) dst[i] = v[a];
+    }
   }
 }
 
@@ -816,12 +833,12 @@ int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st) {
 
 int launch_pad_rows(const void* src0, const void* src1, void* dst0, void* dst1, int rows, int cols, int bf16, hipStream_t st) {
   if (rows <= 0 || cols <= 0) return 0;
-  const int cpr = (cols + 7) / 8;
-  const dim3 grid(rows, src1 ? 2 : 1), block(cpr > 128 ? 256 : 64);
-  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, grid, block, 0, st, (const uint16_t*)src0, (const uint16_t*)src1,
-                               (uint16_t*)dst0, (uint16_t*)dst1, cols, cpr);
-  else hipLaunchKernelGGL(pad_rows_kernel<uint32_t>, grid, block, 0, st, (const uint32_t*)src0, (const uint32_t*)src1,
-                          (uint32_t*)dst0, (uint32_t*)dst1, cols, cpr);
+  if (rows & 7) return -1;
+  const dim3 grid(rows, src1 ? 2 : 1);
+  const int words = (cols + 7) / 8 * (bf16 ? 4 : 8);
+  const uint32_t *s0 = (const uint32_t*)src0, *s1 = (const uint32_t*)src1;
+  if (bf16) hipLaunchKernelGGL(pad_rows_kernel<true>, grid, dim3(256), 0, st, s0, s1, (uint32_t*)dst0, (uint32_t*)dst1, cols, words);
+  else hipLaunchKernelGGL(pad_rows_kernel<false>, grid, dim3(256), 0, st, s0, s1, (uint32_t*)dst0, (uint32_t*)dst1, cols, words);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
