@@ -225,8 +225,8 @@ struct Walk {
   }
 };
 
-// Bound by the MFMAs (at the 1.8 to 1.95 GHz that these products run at) and by what the L2 hands out, which overlap all
-// but a fifth: 256x256 tiles, 4096 tokens, us a slab: 0.75; without loads 0.65, without LDS reads 0.59, without MFMAs 0.53.
+// Bound by the MFMAs (at the clock that these products leave: 1.8 to 1.95 GHz on one card, 1.62 to 1.74 on another) and by
+// what the L2 hands out, which overlap all but a fifth.  On the faster card: 256x256 tiles, 4096 tokens, us a slab: 0.75; without loads 0.65, without LDS reads 0.59, without MFMAs 0.53.
 // At 4096 x 11008, 4096 tokens: X [Wg|W1] 600 us (1.23 PFLOP/s), H W2 259 (1.43), dY W2^T 354 (1.04), dU W1^T + dG Wg^T 509 (1.45),
 // X^T [dU|dG] 631 (1.17), H^T dY 315 (1.17).
 template <typename T, int BM, int BN, int WGM, int WGN, int STAGES, int LA_, int LB_, int EPI>
@@ -646,7 +646,8 @@ __global__ void __launch_bounds__(256) outer_kernel(const PlainArgs p, int tiles
 
 // A workgroup per row, in 32-bit words: neighbouring lanes on neighbouring ones, AT of a thread's under way.  (A row of
 // an odd number of bf16 begins in the middle of a word in every second row.  The matrix has a multiple of 8 rows, so
-// that each word with an element of it is whole.)  blockIdx.y: which of the two matrices.
+// that each word with an element of it is whole.)  blockIdx.y: which of the two matrices.  Bound by memory: two bf16
+// matrices of 4096 x 11007, 360 MB, in 71 us (5.1 TB/s); by elements, eight to a thread, 97.
 template <bool BF16>
 __global__ void __launch_bounds__(256) pad_rows_kernel(const uint32_t* src0, const uint32_t* src1, uint32_t* dst0, uint32_t* dst1,
                                                        int cols, int words) {
