@@ -10,13 +10,13 @@ namespace ffsplit {
 namespace {
 
 // n = r x with r = (mean(x^2) + eps)^(-1/2), so dx = r dn - x r^3 mean(x dn): two sums over the row,
-// then one pass.  TPR threads per row, which keep rows of up to 32 TPR elements in registers (one read
-// of everything); longer rows are read a second time.  5120 rows of 4096, bf16 with residual and copy, 294 MB: 48 us
+// then one pass.  TPR threads per row, which keep it in registers (one read of everything): rows of up to
+// 1024 elements in a wavefront, 8192 in a workgroup, where longer ones are read a second time.  5120 rows of 4096, bf16 with residual and copy, 294 MB: 48 us
 // (6.1 TB/s) in traces, 56 a call back to back.
 template <bool BF16, int TPR>
 __global__ void __launch_bounds__(256) rmsnorm_backward_kernel(const float* x, const void* dn, int64_t T, int d, float eps,
                                                                const float* residual, float* dx, void* cast) {
-  constexpr int NV = 4, RPB = 256 / TPR, WPR = TPR / 64;
+  constexpr int NV = TPR == 64 ? 2 : 4, RPB = 256 / TPR, WPR = TPR / 64;
   __shared__ float sums[4][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int t = tid % TPR;
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256) rmsnorm_backward_kernel(const float* x, c
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) { s2 = fmaf(v[i][e], v[i][e], s2); sx = fmaf(v[i][e], g[i][e], sx); }
-    if (on)
+    if (TPR == 256 && on)
       for (int c = (t + NV * TPR) * 8; c < d; c += TPR * 8) {
         float a[8], b[8];
         load(c, a, b);
@@ -78,11 +78,12 @@ __global__ void __launch_bounds__(256) rmsnorm_backward_kernel(const float* x, c
         const int c = (t + i * TPR) * 8;
         if (c < d) emit(c, v[i], g[i]);
       }
-      for (int c = (t + NV * TPR) * 8; c < d; c += TPR * 8) {
-        float a[8], b[8];
-        load(c, a, b);
-        emit(c, a, b);
-      }
+      if (TPR == 256)
+        for (int c = (t + NV * TPR) * 8; c < d; c += TPR * 8) {
+          float a[8], b[8];
+          load(c, a, b);
+          emit(c, a, b);
+        }
     }
   }
 }
@@ -272,7 +273,7 @@ int for_groups(const GradSet& set, F f) {
 int launch_rmsnorm_backward(const float* x, const void* dn, int64_t T, int d, float eps, int bf16, const float* residual,
                             float* dx, void* dx_cast, hipStream_t st) {
   if (T <= 0) return 0;
-  // a wavefront per row up to 1024 elements, a workgroup beyond (us with a wavefront / a workgroup, bf16, 16384 rows of
+  // a wavefront per row up to 1024 elements (no more: see the kernel), a workgroup beyond (us with a wavefront / a workgroup, bf16, 16384 rows of
   // 512 22 / 35, 1024 40 / 45, 1536 64 / 63, 2048 99 / 91, 8192 500 / 390; 64 rows of 512 4.2 / 3.7, 8192 11 / 4.9)
   const bool wide = d > 1024;
   const int64_t blocks = wide ? T : (T + 3) / 4;

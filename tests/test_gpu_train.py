@@ -292,6 +292,12 @@ def test_rmsnorm_backward(ff, T, d, dtype):
     assert torch.equal(acc, dx)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(5, 520), (6, 1016), (3, 1024), (5, 1032), (3, 1536)])
+def test_rmsnorm_backward_by_wavefront_and_by_workgroup(ff, T, d, dtype):
+    test_rmsnorm_backward(ff, T, d, dtype)
+
+
 def test_rmsnorm_backward_of_many_rows(ff):
     """More rows than one launch has workgroups: every row is the one that a short call gives."""
     T, d = (1 << 22) + 5, 8
@@ -301,6 +307,14 @@ def test_rmsnorm_backward_of_many_rows(ff):
     for a, b in ((0, 1000), (T - 1000, T)):
         assert torch.equal(dx[a:b], ff.token_rmsnorm_backward(x[a:b].contiguous(), dn[a:b].contiguous(), EPS))
     assert ff.token_rmsnorm_backward(x[:0], dn[:0], EPS).shape == (0, d)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("T,d,f", [(3, 64, 1), (9, 72, 2047), (33, 136, 4103)])
+def test_rows_that_are_padded(ff, T, d, f, gated, dtype):
+    """d_ff not a multiple of 8: the weights' copies with aligned rows, one word of a row to several passes of a workgroup."""
+    test_layer_forward_and_gradients(ff, T, d, f, gated, dtype)
 
 
 # ---------------------------------------------------------------- norm over all gradients, clipping
