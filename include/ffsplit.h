@@ -322,9 +322,10 @@ size_t ffsplit_dense_kept_bytes(const ffsplit_desc_t* desc, int64_t T);
  * [T, d_model]; may be the same buffer as Y when Y is fp32.  kept: NULL, or
  * ffsplit_dense_kept_bytes(desc, T) bytes, 256-byte aligned, written for ffsplit_dense_backward (private
  * layout).  Accumulation in fp32; H is rounded to desc->dtype between the two products.  The kept
- * derivatives are fp32 in fp32 layers and fp16 in bf16 layers (finer than bf16; one beyond 65504, which
- * takes a pre-activation of that size, is kept as infinity and makes the gradients behind it non-finite;
- * steps of 6e-8 below 6e-5).  The activation's forms here: GeLU by the rational form 7.1.26 of Abramowitz and
+ * derivatives are fp32 in fp32 layers and 16 bits in bf16 layers (relative error at most 2^-10 from 2^-44
+ * to 65504, finer than bf16; 2^-8 down to 2^-48, and less below, to zero at 2^-66; one beyond 65504, which
+ * takes a pre-activation of that size, is kept as infinity and makes the gradients behind it non-finite).
+ * The activation's forms here: GeLU by the rational form 7.1.26 of Abramowitz and
  * Stegun (absolute error of Phi below 1e-7) in bf16, erff in fp32.
  * workspace: ffsplit_workspace_bytes(desc, FFSPLIT_WS_DENSE_FORWARD, T).
  */

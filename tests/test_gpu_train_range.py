@@ -34,3 +34,64 @@ def test_rmsnorm_backward_wherever_the_norm_itself_is_defined(ff, d, dtype):
     dx = ff.token_rmsnorm_backward(torch.from_numpy(x).cuda(), dn, eps)
     want = orc.token_rmsnorm_backward(x, dnh, eps)
     tu.assert_within(gu.host(dx), want, ((2 * tu.g(d) + 8 * 2.0 ** -24) * m, tu.U["f32"]), f"rmsnorm backward {d} {dtype}")
+
+
+# ---------------------------------------------------------------- the kept derivatives of a bf16 layer
+
+@pytest.mark.parametrize("which", ["tokens", "up", "gate"])
+@pytest.mark.parametrize("log2", [-17, -20, -24, -34, 8])
+def test_small_and_large_factors_keep_their_precision(ff, which, log2, monkeypatch):
+    """Tokens or weights of any size: the factors dH/dU, dH/dG follow them, with a relative error of at most 2^-10."""
+    T, d, f = 33, 64, 203
+    host = list(tu.make_layer(np.random.default_rng(40), d, f, True, T, "bf16"))
+    i = ("tokens", "up", "gate").index(which)
+    host[i] = host[i] * np.float32(2.0 ** log2)
+    X, W1, Wg, W2, dY = host
+    desc = ff.make_desc(d, f, "swiglu", "bf16")
+    dev = tu.to_dev(host, "bf16")
+    _, kept = ff.dense_forward(desc, *dev[:4], want_saved=True)
+    dX, g = ff.dense_backward(desc, *dev[:4], kept, dev[4])
+    _, tape = orc.dense_forward(X, W1, Wg, W2)
+    want_dX, want = orc.dense_backward(X, W1, Wg, W2, tape, dY)
+    monkeypatch.setitem(tu.UD, tu.U["bf16"], (2.0 ** -10, 0.0))
+    b = tu.dense_bounds(X, W1, Wg, W2, tape, dY, tu.U["bf16"], tu.U["bf16"])
+    for name, got, ref in [("dX", dX, want_dX)] + [(k, g[k], want[k]) for k in ("W1", "Wg", "W2")]:
+        tu.assert_within(gu.host(got), ref, b[name], f"{which} 2^{log2} {name}")
+        assert gu.relf(gu.host(got), ref) < gu.TOL["bf16"], (which, log2, name)
+
+
+def _one_to_one(ff, act, dtype, z, u=None):
+    """A layer whose neuron j sees exactly z[j] (and u[j]): returns H and what the backward pass multiplies dH = 1 with."""
+    d = f = len(z)
+    zero = np.zeros((d, f))
+    X, dY = np.zeros((1, d)), np.ones((1, d))
+    X[0, 0] = 1.0
+    Wz, Wu = zero.copy(), zero.copy()
+    Wz[0] = z
+    if u is not None:
+        Wu[0] = u
+    W1, Wg = (Wz, None) if u is None else (Wu, Wz)
+    desc = ff.make_desc(d, f, act, dtype)
+    dev = [gu.dev(a, dtype) for a in (X, W1, Wg, np.eye(d), dY)]
+    Y, kept = ff.dense_forward(desc, *dev[:4], want_saved=True, y_f32=True)
+    _, g = ff.dense_backward(desc, *dev[:4], kept, dev[4], grad_f32=True)
+    return gu.host(Y)[0], gu.host(g["W1"])[0], None if u is None else gu.host(g["Wg"])[0]
+
+
+def test_kept_factors_from_the_smallest_to_the_largest(ff):
+    """dH/dU = silu(z) for z from 2^-60 to 65504, through dU's own rounding to bf16."""
+    import workloads as wl
+    z = wl.bf16_round(np.exp2(np.linspace(-60, 15.9, 128)).astype(np.float32)).astype(np.float64)
+    z[1::2] *= -1
+    z[5], z[7] = 0.0, -65280.0
+    H, dU, dG = _one_to_one(ff, "swiglu", "bf16", z, np.ones(128))
+    s = 1 / (1 + np.exp(-np.clip(z, -600, 600)))
+    silu, slope = z * s, s * (1 + z * (1 - s))
+    # factor, dU, and the sigmoid's own error (an exponential and a reciprocal of a few units, e^-z off by |z| 2^-23)
+    act = (np.minimum(np.abs(z), 200) + 8) * 2.0 ** -23
+    kept = np.where(np.abs(silu) >= 2.0 ** -44, 2.0 ** -10, np.where(np.abs(silu) >= 2.0 ** -48, 2.0 ** -8, 1.0))
+    assert (np.abs(dU - silu) <= (1.01 * (2.0 ** -8 + kept) + act) * np.abs(silu) + 2.0 ** -66).all()
+    assert dU[5] == 0.0 and np.isfinite(dU).all()
+    assert (np.abs(dG - slope) <= (1.01 * (2.0 ** -8 + 2.0 ** -10)) * np.abs(slope) + 2e-6 * (1 + np.minimum(np.abs(z), 200))).all()
+    H, dU, _ = _one_to_one(ff, "swiglu", "bf16", np.array([1e-3, 65536.0, 1e9, 1.0, 2.0, 3.0, 4.0, 5.0]), np.ones(8))
+    assert np.isfinite(H).all() and list(np.isfinite(dU)) == [True, False, False] + [True] * 5
