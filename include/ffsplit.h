@@ -326,7 +326,7 @@ size_t ffsplit_dense_kept_bytes(const ffsplit_desc_t* desc, int64_t T);
  * to 65504, finer than bf16; 2^-8 down to 2^-48, and less below, to zero at 2^-66; one beyond 65504, which
  * takes a pre-activation of that size, is kept as infinity and makes the gradients behind it non-finite).
  * The activation's forms here: GeLU by the rational form 7.1.26 of Abramowitz and
- * Stegun (absolute error of Phi below 1e-7) in bf16, erff in fp32.
+ * Stegun (absolute error of Phi below 1e-7) in bf16, Phi(z) = erfc(-z / sqrt 2) / 2 in fp32.
  * workspace: ffsplit_workspace_bytes(desc, FFSPLIT_WS_DENSE_FORWARD, T).
  */
 int ffsplit_dense_forward(const ffsplit_desc_t* desc, const void* X, int64_t T,

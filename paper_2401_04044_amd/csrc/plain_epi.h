@@ -22,7 +22,7 @@ __device__ __forceinline__ float sigmoid_of(float z) {
 // gelu(z) = z Phi(z) and gelu'(z) = Phi(z) + z phi(z).  bf16 layers: Phi(-a) = e^(-a^2/2) / 2 * p(t),
 // t = 1 / (1 + 0.3275911 a / sqrt 2), the rational form 7.1.26 of Abramowitz and Stegun (absolute
 // error 1.5e-7 of erf): its exponential is phi's, so that both cost one exponential and one
-// reciprocal.  fp32 layers: erff and expf.
+// reciprocal.  fp32 layers: erfcf and expf.
 template <typename T>
 __device__ __forceinline__ void gelu_and_slope(float z, float& h, float& d) {
   if (sizeof(T) == 2) {
@@ -38,7 +38,7 @@ __device__ __forceinline__ void gelu_and_slope(float z, float& h, float& d) {
     h = z * cdf;
     d = fmaf(z * 0.39894228f, e, cdf);
   } else {
-    const float cdf = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    const float cdf = 0.5f * erfcf(z * -0.70710678118654752f);   // (1 + erf cancels below 0: nothing is left at -5.6)
     h = z * cdf;
     d = cdf + z * (0.39894228040143268f * expf(-0.5f * z * z));
   }

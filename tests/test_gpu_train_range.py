@@ -95,3 +95,32 @@ def test_kept_factors_from_the_smallest_to_the_largest(ff):
     assert (np.abs(dG - slope) <= (1.01 * (2.0 ** -8 + 2.0 ** -10)) * np.abs(slope) + 2e-6 * (1 + np.minimum(np.abs(z), 200))).all()
     H, dU, _ = _one_to_one(ff, "swiglu", "bf16", np.array([1e-3, 65536.0, 1e9, 1.0, 2.0, 3.0, 4.0, 5.0]), np.ones(8))
     assert np.isfinite(H).all() and list(np.isfinite(dU)) == [True, False, False] + [True] * 5
+
+
+# ---------------------------------------------------------------- GeLU's lower tail
+
+def _phi(z):
+    import math
+    return np.array([0.5 * math.erfc(-t / math.sqrt(2.0)) for t in z]), np.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+
+
+def test_gelu_in_fp32_is_accurate_in_its_tail(ff):
+    """z from -12 to 4.  The arguments of erfc and exp are off by 2^-23 of z / sqrt 2 and z^2 / 2, which moves either by
+    z^2 2^-23 of its value at most; the functions themselves and the products add less than 32 units."""
+    z = np.linspace(-12, 4, 256).astype(np.float32).astype(np.float64)
+    H, slope, _ = _one_to_one(ff, "gelu", "f32", z)
+    cdf, phi = _phi(z)
+    tol = (2 * z * z + 32) * 2.0 ** -23
+    assert (np.abs(H - z * cdf) <= tol * np.abs(z * cdf)).all()
+    # (the slope is a difference of two such terms below zero)
+    assert (np.abs(slope - (cdf + z * phi)) <= tol * (cdf + np.abs(z) * phi)).all()
+
+
+def test_gelu_in_bf16_in_its_tail(ff):
+    """Phi is off by 1e-7 at most, everywhere; H and the kept slope are rounded to bf16 and to 2^-10."""
+    import workloads as wl
+    z = wl.bf16_round(np.linspace(-12, 4, 256).astype(np.float32)).astype(np.float64)
+    H, slope, _ = _one_to_one(ff, "gelu", "bf16", z)
+    cdf, phi = _phi(z)
+    assert (np.abs(H - z * cdf) <= 2.0 ** -8 * np.abs(z * cdf) + 1.01e-7 * np.abs(z)).all()
+    assert (np.abs(slope - (cdf + z * phi)) <= 1.01 * (2.0 ** -8 + 2.0 ** -10) * np.abs(cdf + z * phi) + 2e-7 * (1 + np.abs(z))).all()
