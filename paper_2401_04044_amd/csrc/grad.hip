@@ -200,7 +200,11 @@ __global__ void __launch_bounds__(256) grad_norm_finish_kernel(const double* par
 // so that it stays there: 541 MB read and written in 185 us, norm and clipping together 312 -> 280.
 __global__ void __launch_bounds__(256) grad_clip_kernel(const Group g, const float* norm, float max_norm) {
   const float n = *norm;
-  const float k = __builtin_isfinite(n) && n > max_norm ? max_norm / n : 1.0f;
+  float k = __builtin_isfinite(n) && n > max_norm ? max_norm / n : 1.0f, p = 1.0f;
+  if (k < 0x1p-126f) {   // a subnormal factor has lost its last bits: in two parts, the first a power of two near 1 / n
+    p = ldexpf(1.0f, -min(ilogbf(n), 126));
+    k = max_norm / (n * p);
+  }
   const int chunks = g.first[g.n];
   for (int r = blockIdx.x; r < chunks; r += gridDim.x) {
     const int c = chunks - 1 - r;
@@ -208,13 +212,13 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const Group g, const flo
     const int64_t at = (int64_t)(c - g.first[i]) * CHUNK;
     const char* const src = (const char*)g.src[i] + at;
     char* const dst = (char*)g.dst[i] + at;
-    if (k == 1.0f && src == dst) continue;   // in place, nothing to scale
+    if (k == 1.0f && p == 1.0f && src == dst) continue;   // in place, nothing to scale
     const int left = (int)min((int64_t)CHUNK, g.bytes[i] - at);
     const bool f32 = (g.f32 >> i) & 1;
     auto scale = [&](uint32_t u) -> uint32_t {
-      if (k == 1.0f) return u;   // (a copy, NaN payloads and all)
-      if (f32) return __float_as_uint(__uint_as_float(u) * k);
-      return pack_bf16x2(__uint_as_float(u << 16) * k, __uint_as_float(u & 0xffff0000u) * k);
+      if (k == 1.0f && p == 1.0f) return u;   // (a copy, NaN payloads and all)
+      if (f32) return __float_as_uint(__uint_as_float(u) * p * k);
+      return pack_bf16x2(__uint_as_float(u << 16) * p * k, __uint_as_float(u & 0xffff0000u) * p * k);
     };
     if (left == CHUNK) {
       u32x4_t v[CHUNK / 4096];

@@ -124,3 +124,25 @@ def test_gelu_in_bf16_in_its_tail(ff):
     cdf, phi = _phi(z)
     assert (np.abs(H - z * cdf) <= 2.0 ** -8 * np.abs(z * cdf) + 1.01e-7 * np.abs(z)).all()
     assert (np.abs(slope - (cdf + z * phi)) <= 1.01 * (2.0 ** -8 + 2.0 ** -10) * np.abs(cdf + z * phi) + 2e-7 * (1 + np.abs(z))).all()
+
+
+# ---------------------------------------------------------------- clipping
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("limit", [1.0, 1e-6, 1e-20, 1e-35, 2.0 ** -126])
+def test_clipping_by_a_factor_below_the_normal_numbers(ff, limit, dtype):
+    """Gradients of 1e35 and 1e20 scaled by max_norm / norm, which is subnormal or less: the results are ordinary numbers."""
+    g = torch.full((4099,), 1e35, dtype=gu.TDT[dtype], device="cuda")
+    g[::3] = -1e20
+    g[1] = 0.0
+    host = gu.host(g)
+    norm, flag, (out,) = ff.clip_grad_norm([g.clone()], limit)
+    limit = float(np.float32(limit))
+    want = host * (limit / orc.grad_norm([host]))
+    # the norm, the factor and the product are rounded to fp32 (at their subnormal end by half of 2^-149), the result to its type
+    step = 2.0 ** -149 if dtype == "f32" else 2.0 ** -133
+    assert int(flag) == 0
+    assert (np.abs(gu.host(out) - want) <= (3 * 2.0 ** -24 + tu.U[dtype]) * np.abs(want) + step).all()
+    # in two halves, into other buffers: the same bits
+    two = ff.grad_clip([g[:2048], g[2048:]], norm, limit, out=[torch.empty_like(g[:2048]), torch.empty_like(g[2048:])])
+    assert torch.equal(torch.cat(two), out)
