@@ -308,10 +308,15 @@ __global__ void __launch_bounds__(256) token_rmsnorm_kernel(const float* x, int 
 }
 
 int launch_token_rmsnorm(const float* x, int64_t T, int d, float eps, int bf16, void* out, hipStream_t st) {
-  if (T <= 0) return 0;
-  if (bf16) hipLaunchKernelGGL(token_rmsnorm_kernel<true>, dim3((unsigned)T), dim3(256), 0, st, x, d, eps, out);
-  else hipLaunchKernelGGL(token_rmsnorm_kernel<false>, dim3((unsigned)T), dim3(256), 0, st, x, d, eps, out);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  constexpr int64_t ROWS = 1 << 23;   // of one launch, which has at most 2^32 threads
+  for (int64_t t = 0; t < T; t += ROWS) {
+    const dim3 grid((unsigned)(T - t < ROWS ? T - t : ROWS));
+    const float* const in = x + t * d;
+    if (bf16) hipLaunchKernelGGL(token_rmsnorm_kernel<true>, grid, dim3(256), 0, st, in, d, eps, (bf16_t*)out + t * d);
+    else hipLaunchKernelGGL(token_rmsnorm_kernel<false>, grid, dim3(256), 0, st, in, d, eps, (float*)out + t * d);
+    if (hipGetLastError() != hipSuccess) return -1;
+  }
+  return 0;
 }
 
 // packed[i] = b1[idx[i]] for i < k, 0 up to kp; packed[kp + i] = b1[rest[i]] for i < m, 0 up to kp + mp
