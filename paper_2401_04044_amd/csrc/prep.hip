@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(256) token_rmsnorm_kernel(const float* x, int 
   for (int i = 0; i < NV; ++i) {
     s = fmaf(v[i].x, v[i].x, s); s = fmaf(v[i].y, v[i].y, s); s = fmaf(v[i].z, v[i].z, s); s = fmaf(v[i].w, v[i].w, s);
   }
-  for (int c = tid * 4 + NV * 1024; c < d; c += 1024) {
+  for (int64_t c = tid * 4 + NV * 1024; c < d; c += 1024) {   // (64 bits: d may end 8 below 2^31)
     const float4 w = *(const float4*)(row + c);
     s = fmaf(w.x, w.x, s); s = fmaf(w.y, w.y, s); s = fmaf(w.z, w.z, s); s = fmaf(w.w, w.w, s);
   }
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(256) token_rmsnorm_kernel(const float* x, int 
   __syncthreads();
   const float tot = ((wsum[0] + wsum[1]) + wsum[2]) + wsum[3];
   const float inv = 1.0f / sqrtf(tot / (float)d + eps);
-  auto emit = [&](int c, const float4& w) {
+  auto emit = [&](int64_t c, const float4& w) {
     if (BF16) {
       *(uint2*)((bf16_t*)out + (int64_t)blockIdx.x * d + c) =
           make_uint2(pack_bf16x2(w.x * inv, w.y * inv), pack_bf16x2(w.z * inv, w.w * inv));
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(256) token_rmsnorm_kernel(const float* x, int 
     const int c = tid * 4 + i * 1024;
     if (c < d) emit(c, v[i]);
   }
-  for (int c = tid * 4 + NV * 1024; c < d; c += 1024) emit(c, *(const float4*)(row + c));
+  for (int64_t c = tid * 4 + NV * 1024; c < d; c += 1024) emit(c, *(const float4*)(row + c));
 }
 
 int launch_token_rmsnorm(const float* x, int64_t T, int d, float eps, int bf16, void* out, hipStream_t st) {

@@ -48,3 +48,11 @@ def test_a_stack_trained_on_more_than_2_to_24_tokens(ff):
         total = part if total is None else {k: total[k] + part[k] for k in part}
     for k in whole:    # fp32 sums of 2^19 matrix instructions in other orders: 2^9.5 half steps as they add up at random
         assert float((total[k] - whole[k]).norm() / whole[k].norm()) < 2.0 ** -12, k
+
+
+def test_the_norm_of_the_longest_row(ff):
+    """The last columns of a row of 2^31 - 8: a 31-bit column index would have wrapped."""
+    d = (1 << 31) - 8
+    x = torch.ones(1, d, device="cuda")
+    n = ff.token_rmsnorm(x)
+    assert bool((n[:, -3000:] == 1).all()) and bool((n[:, ::4099] == 1).all())
