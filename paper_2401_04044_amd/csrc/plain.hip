@@ -66,11 +66,12 @@ constexpr uint32_t FAR = 1u << 30;          // a resource is set anew before a s
 // 16 bytes per lane from the buffer r at offset + soff (zeros beyond its end) straight into LDS, lane l to
 // dst + 16 l; r, dst and soff in scalar registers.  In assembly because the compiler, when it sees a load
 // into LDS, waits for all of them before every turned-round LDS read; here the counts are kept by hand.
-// (The s_nop covers m0, which nothing else in these kernels uses.)
+// (dst goes into m0, which the compiler writes: it then knows what m0 holds.  The s_nop is the distance that a load needs
+// from that write.)
 __device__ __forceinline__ void load_to_lds(const u32x4_t& r, uint32_t dst, uint32_t offset, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen lds"
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %3 offen lds"
                :
-               : "v"(offset), "s"(r), "s"(dst), "s"(soff)
+               : "v"(offset), "s"(r), "{m0}"(dst), "s"(soff)
                : "memory");
 }
 // A buffer resource for what lies from base on, `left` bytes, in scalar registers.  (The s_nop keeps the
