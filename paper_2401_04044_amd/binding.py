@@ -407,6 +407,18 @@ def _grads_for(desc, grads, accumulate, grad_f32, device, what=""):
     return {k: grads.get(k) for k in shapes}
 
 
+def _grads_apart(written, others):
+    """A gradient's buffer is written once, and while the call still reads the other tensors."""
+    spans = sorted([(t.data_ptr(), t.nbytes, 1) for t in written] + [(t.data_ptr(), t.nbytes, 0) for t in others])
+    end = end_written = 0       # of what begins further in front
+    for at, n, is_written in spans:
+        if at < (end if is_written else end_written):
+            raise ValueError("gradients: a buffer that overlaps another tensor of the call")
+        end = max(end, at + n)
+        if is_written:
+            end_written = max(end_written, at + n)
+
+
 def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=None, accumulate=False, grad_f32=False,
                    workspace=None):
     """Backward pass of dense_forward.  Returns (dX or None, {"W1", "Wg", "W2": gradients or None})."""
@@ -415,12 +427,17 @@ def dense_backward(desc, X, W1, Wg, W2, saved, dY, dX=None, want_dx=True, grads=
     _take_layer(desc, W1, Wg, W2, dev)
     _take(dY, "dY", (T, desc.d_model), dt, dev)
     _take_kept(saved, dense_kept_bytes(desc, T), dev)
+    mine = [] if dX is None else [dX]
     if dX is None and want_dx:
         dX = torch.empty((T, desc.d_model), dtype=dt, device=dev)
     _take(dX, "dX", (T, desc.d_model), dt, dev)
     if dX is not None and T and dX.data_ptr() in (dY.data_ptr(), X.data_ptr()):
         raise ValueError("dX: the buffer of dY or X, which the weights' gradients read behind it")
     g = _grads_for(desc, grads, accumulate, grad_f32, dev)
+    if grads is not None:
+        mine += [t for t in g.values() if t is not None]
+    if mine and T:
+        _grads_apart(mine, [t for t in (dY, X, W1, Wg, W2, saved) if t is not None])
     with _on(dev):
         ws = _scratch(workspace_bytes(desc, WS_DENSE_BACKWARD, T), workspace, dev)
         rc = lib.ffsplit_dense_backward(ctypes.byref(desc), _ptr(X), T, _ptr(W1), _ptr(Wg), _ptr(W2), _ptr(saved), _ptr(dY),
@@ -575,6 +592,9 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
     written = [t.data_ptr() for q in g for t in q.values() if t is not None]
     if len(set(written)) != len(written):
         raise ValueError("gradients: a buffer is listed twice")
+    if grads is not None:
+        _grads_apart([t for q in g for t in q.values() if t is not None],
+                     [t for W in layers for t in W.values() if t is not None] + [saved, dx])
     W1, Wg, W2 = _stack_args(desc, layers, dev)
     gated = desc.act == ACT_SWIGLU
     with _on(dev):

@@ -1,0 +1,42 @@
+"""What the training calls refuse beyond single bad arguments (host only, no GPU)."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2401_04044_amd as ff
+
+
+def _layer(T=100, d=64, f=100, act="swiglu"):
+    """T = d_ff, so that a token matrix has the shape of W2's gradient."""
+    desc = ff.make_desc(d, f, act, "f32")
+    return desc, dict(X=torch.zeros(T, d), W1=torch.zeros(d, f), Wg=torch.zeros(d, f), W2=torch.zeros(f, d),
+                      saved=torch.zeros(ff.dense_kept_bytes(desc, T), dtype=torch.uint8), dY=torch.zeros(T, d))
+
+
+def test_a_gradients_buffer_is_nothing_else_of_the_call():
+    desc, t = _layer()
+    one, two = torch.zeros(64, 100), torch.zeros(100, 64)
+    flat = torch.zeros(2 * 6400)
+    for W1, Wg in ((one, one), (flat[:6400].view(64, 100), flat[6396:-4].view(64, 100)), (flat[4:6404].view(64, 100), flat[:6400].view(64, 100))):
+        with pytest.raises(ValueError, match="overlaps"):
+            ff.dense_backward(desc, **t, grads={"W1": W1, "Wg": Wg, "W2": two})
+    for k, other in (("W2", "X"), ("W2", "dY"), ("W1", "W1"), ("Wg", "W1"), ("W2", "W2")):
+        with pytest.raises(ValueError, match="overlaps"):
+            ff.dense_backward(desc, **t, grads={k: t[other]})
+    with pytest.raises(ValueError, match="overlaps"):
+        ff.dense_backward(desc, **t, dX=two, grads={"W2": two})
+    both = torch.zeros(150, 64)
+    with pytest.raises(ValueError, match="overlaps"):
+        ff.dense_backward(desc, **dict(t, dY=both[:100]), dX=both[50:])
+    # side by side is fine: the call gets as far as asking for a GPU
+    with pytest.raises(ValueError, match="GPU"):
+        ff.dense_backward(desc, **t, grads={"W1": flat[:6400].view(64, 100), "Wg": flat[6400:].view(64, 100), "W2": two})
+    layers = [{k: torch.zeros_like(t[k]) for k in ("W1", "Wg", "W2")} for _ in range(2)]
+    saved = torch.zeros(1 << 20, dtype=torch.uint8)
+    for bad in (layers[0]["W2"], layers[1]["W2"], t["dY"]):
+        grads = [{k: torch.zeros_like(W[k]) for k in W} for W in layers]
+        grads[1]["W2"] = bad
+        with pytest.raises(ValueError, match="overlaps"):
+            ff.dense_stack_backward(desc, layers, saved, t["dY"], grads=grads)
