@@ -484,6 +484,7 @@ class _GradList:
             ptrs.append(g.data_ptr())
             counts.append(g.numel())
             dtypes.append(F32 if dt == torch.float32 else BF16)
+        self._read = set(ptrs)
         self.ptrs, self.counts = (ctypes.c_void_p * max(n, 1))(*ptrs), (ctypes.c_int64 * max(n, 1))(*counts)
         self.dtypes = (ctypes.c_int32 * max(n, 1))(*dtypes)
 
@@ -499,6 +500,8 @@ class _GradList:
                 raise ValueError("out: tensors like the gradients are wanted, contiguous and on their device")
             ptrs.append(o.data_ptr())
         self._apart(ptrs)
+        if not self._read.isdisjoint(ptrs) and any(p in self._read and p != q for p, q, c in zip(ptrs, self.ptrs, self.counts) if c):
+            raise ValueError("out: the buffer of another gradient, which is still read")
         return (ctypes.c_void_p * max(self.n, 1))(*ptrs)
 
     def _apart(self, ptrs):

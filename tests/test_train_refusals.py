@@ -40,3 +40,18 @@ def test_a_gradients_buffer_is_nothing_else_of_the_call():
         grads[1]["W2"] = bad
         with pytest.raises(ValueError, match="overlaps"):
             ff.dense_stack_backward(desc, layers, saved, t["dY"], grads=grads)
+
+
+def test_clipped_gradients_do_not_go_where_another_one_lies():
+    a, b, c, one = torch.ones(8), torch.ones(8), torch.ones(8), torch.ones(1)
+    for out in ([b, a], [b, c], [c, a]):
+        with pytest.raises(ValueError, match="still read"):
+            ff.grad_clip([a, b], one, 1.0, out=out)
+        with pytest.raises(ValueError, match="still read"):
+            ff.clip_grad_norm([a, b], 1.0, out=out)
+    for out in ([a, c], [c, b], [a, b], None):          # in place, or elsewhere: as far as asking for a GPU
+        with pytest.raises(ValueError, match="GPU"):
+            ff.grad_clip([a, b], one, 1.0, out=out)
+    e = torch.ones(8)[:0]
+    with pytest.raises(ValueError, match="GPU"):
+        ff.grad_clip([a, e, e], one, 1.0, out=[a, e, e])
