@@ -404,7 +404,7 @@ int ffsplit_dense_stack_forward(const ffsplit_desc_t* desc, int32_t n_layers, co
  * return that of the stream in front of the first.  dW1, dWg, dW2: HOST arrays of n_layers device pointers
  * that receive the weights' gradients (flags as for ffsplit_dense_backward).  If norm is not NULL the norm
  * over all of them goes to *norm and *nonfinite (ffsplit_grad_norm; nonfinite may be NULL), and if also
- * max_norm > 0 they are clipped in place (ffsplit_grad_clip).
+ * max_norm > 0 they are clipped in place (ffsplit_grad_clip; 0 or less: not; NaN is refused).
  * workspace: as for the forward pass.
  */
 int ffsplit_dense_stack_backward(const ffsplit_desc_t* desc, int32_t n_layers, const void* const* W1,

@@ -360,7 +360,7 @@ int ffsplit_dense_stack_backward(const ffsplit_desc_t* d, int32_t n_layers, cons
   if (rc) return rc;
   if (flags & ~(FFSPLIT_GRAD_F32 | FFSPLIT_GRAD_ACCUMULATE)) return FFSPLIT_E_BADDESC;
   if (((uintptr_t)norm & 3u) || ((uintptr_t)nonfinite & 3u)) return FFSPLIT_E_ALIGN;
-  if (n_layers > 0x7fffffff / 3) return FFSPLIT_E_BADSHAPE;
+  if (n_layers > 0x7fffffff / 3 || max_norm != max_norm) return FFSPLIT_E_BADSHAPE;
   // (the norm's partial sums lie where the layers' scratch was)
   if (!workspace || workspace_bytes < stack_ws(*d, T) ||
       (norm && workspace_bytes < grad_norm_ws_bytes((int64_t)3 * n_layers)))

@@ -55,3 +55,17 @@ def test_clipped_gradients_do_not_go_where_another_one_lies():
     e = torch.ones(8)[:0]
     with pytest.raises(ValueError, match="GPU"):
         ff.grad_clip([a, e, e], one, 1.0, out=[a, e, e])
+
+
+def test_a_limit_that_is_not_a_number_is_refused():
+    """A limit that a program computed to NaN would otherwise leave the gradients of a step unclipped."""
+    desc = ff.make_desc(64, 100, "gelu", "f32")
+    at = ctypes.c_void_p(0x1000)      # aligned, never dereferenced: the calls fail validation, or have nothing to launch
+    p = (ctypes.c_void_p * 1)(0x1000)
+
+    def call(max_norm, layers=1):
+        return ff.lib.ffsplit_dense_stack_backward(ctypes.byref(desc), layers, p, None, p, at, at, 4, 1e-6, p, None, p, 0, max_norm,
+                                                   None, None, at, 1 << 40, None)
+
+    assert call(math.nan) == -3 and call(math.nan, 0) == -3
+    assert call(0.0, 0) == 0 and call(-1.0, 0) == 0 and call(math.inf, 0) == 0
