@@ -314,6 +314,16 @@ def _take(t, what, shape, dtype, device):
     return t
 
 
+def _no_graph(**tensors):
+    """The calls are not recorded by autograd: a graph that leads into one would end there unnoticed, and a write into a
+    tensor of a graph would not be noticed either.  (Weights may be parameters: their gradients are dense_backward's.)"""
+    if torch.is_grad_enabled():
+        for what, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{what}: requires grad, but the call is not recorded: detach it and take its gradient from the "
+                                 "backward call")
+
+
 _HERE_ALREADY = contextlib.nullcontext()
 
 
@@ -358,7 +368,9 @@ def dense_kept_bytes(desc, T):
 
 def dense_forward(desc, X, W1, Wg, W2, Y=None, residual=None, y_f32=False, want_saved=False, saved=None, workspace=None):
     """The uncompressed layer on plain weights: Y = [residual +] act(X W1, X Wg) W2.  Returns Y, or (Y, saved)
-    with want_saved or a buffer for it: what dense_backward needs."""
+    with want_saved or a buffer for it: what dense_backward needs.  Not recorded by autograd (dense_backward gives the
+    gradients): X, residual and Y that require grad are refused while it records, weights may be parameters."""
+    _no_graph(X=X, residual=residual, Y=Y)
     T, dev, dt = X.shape[0], X.device, _DTYPES[desc.dtype]
     _take(X, "X", (T, desc.d_model), dt, dev)
     _take_layer(desc, W1, Wg, W2, dev)
@@ -563,7 +575,8 @@ def _stack_args(desc, layers, device):
 
 def dense_stack_forward(desc, layers, x, eps=1e-6, want_saved=False, saved=None, workspace=None):
     """x <- x + FFN_l(n(x)) for every layer (dicts W1, Wg, W2), in place on the fp32 stream x [T, d].  Returns x, or
-    what dense_stack_backward needs with want_saved or a buffer for it."""
+    what dense_stack_backward needs with want_saved or a buffer for it.  Not recorded by autograd, as dense_forward."""
+    _no_graph(x=x)
     n, T, dev = len(layers), x.shape[0], x.device
     _take(x, "x", (T, desc.d_model), torch.float32, dev)
     keep = want_saved or saved is not None

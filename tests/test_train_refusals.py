@@ -69,3 +69,23 @@ def test_a_limit_that_is_not_a_number_is_refused():
 
     assert call(math.nan) == -3 and call(math.nan, 0) == -3
     assert call(0.0, 0) == 0 and call(-1.0, 0) == 0 and call(math.inf, 0) == 0
+
+
+def test_a_graph_does_not_end_in_a_call_unnoticed():
+    """Tokens that require grad would give an output that does not; parameters as weights are the ordinary case."""
+    desc, t = _layer(T=4, act="gelu")
+    W1, W2 = torch.nn.Parameter(t["W1"]), torch.nn.Parameter(t["W2"])
+    X = torch.zeros(4, 64, requires_grad=True)
+    res, Y = torch.zeros(4, 64, requires_grad=True), torch.zeros(4, 64, requires_grad=True)
+    for kw in (dict(X=X), dict(X=X * 2), dict(X=t["X"], residual=res, y_f32=True), dict(X=t["X"], Y=Y)):
+        with pytest.raises(ValueError, match="requires grad"):
+            ff.dense_forward(desc, W1=W1, Wg=None, W2=W2, **kw)
+    with pytest.raises(ValueError, match="requires grad"):
+        ff.dense_stack_forward(desc, [{"W1": W1, "W2": W2}], X * 2)
+    # as far as asking for a GPU
+    with pytest.raises(ValueError, match="GPU"):
+        ff.dense_forward(desc, X.detach(), W1, None, W2)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+        ff.dense_forward(desc, X, W1, None, W2)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+        ff.dense_stack_forward(desc, [{"W1": W1, "W2": W2}], X)
