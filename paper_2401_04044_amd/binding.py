@@ -595,9 +595,11 @@ def dense_stack_forward(desc, layers, x, eps=1e-6, want_saved=False, saved=None,
 
 
 def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumulate=False, grad_f32=False, max_norm=0.0,
-                         workspace=None):
+                         workspace=None, want_norm=True):
     """Backward pass of dense_stack_forward, in place on the stream's gradient dx [T, d].  Returns (gradients: a dict
-    W1, Wg, W2 per layer; their norm [1]; its flag [1]); with max_norm > 0 the gradients are clipped."""
+    W1, Wg, W2 per layer; their norm [1]; its flag [1]); with max_norm > 0 the gradients are clipped.  grads: dicts of
+    buffers, one for every weight.  Without want_norm (all but the last of accumulated micro-batches) the gradients are
+    not read again, and norm and flag are None."""
     n, T, dev = len(layers), dx.shape[0], dx.device
     _take(dx, "dx", (T, desc.d_model), torch.float32, dev)
     _take_kept(saved, int(lib.ffsplit_dense_stack_kept_bytes(ctypes.byref(desc), n, T)), dev)
@@ -611,11 +613,13 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
     if grads is not None:
         _grads_apart([t for q in g for t in q.values() if t is not None],
                      [t for W in layers for t in W.values() if t is not None] + [saved, dx])
+    if max_norm > 0 and not want_norm:
+        raise ValueError("max_norm: clipping needs the norm")
     W1, Wg, W2 = _stack_args(desc, layers, dev)
     gated = desc.act == ACT_SWIGLU
     with _on(dev):
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
-        flag = torch.empty(1, dtype=torch.int32, device=dev)
+        norm = torch.empty(1, dtype=torch.float32, device=dev) if want_norm else None
+        flag = torch.empty(1, dtype=torch.int32, device=dev) if want_norm else None
         need = max(workspace_bytes(desc, WS_DENSE_STACK, T), int(lib.ffsplit_workspace_bytes(None, WS_GRAD_NORM, 3 * n)))
         ws = _scratch(need, workspace, dev)
         rc = lib.ffsplit_dense_stack_backward(ctypes.byref(desc), n, W1, Wg, W2, _ptr(saved), _ptr(dx), T,

@@ -89,3 +89,10 @@ def test_a_graph_does_not_end_in_a_call_unnoticed():
         ff.dense_forward(desc, X, W1, None, W2)
     with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
         ff.dense_stack_forward(desc, [{"W1": W1, "W2": W2}], X)
+
+
+def test_clipping_without_the_norm_is_refused():
+    desc, t = _layer(T=4, act="gelu")
+    saved = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="needs the norm"):
+        ff.dense_stack_backward(desc, [{"W1": t["W1"], "W2": t["W2"]}], saved, t["dY"], max_norm=1.0, want_norm=False)
