@@ -2,23 +2,9 @@
 // launches store.
 #pragma once
 #include "common.h"
+#include "plain_plan.h"
 
 namespace ffsplit {
-
-// What a product does with its sums (Z, U: sums of the gate and up columns, S: of the only ones):
-//   EPI_OUT   C = S [+ resid] [+ C], in the storage type or fp32
-//   EPI_GLU   H = silu(Z) U, and if D1 is set D1 = dH/dU = silu(Z), D2 = dH/dZ = U silu'(Z)
-//   EPI_GELU  H = gelu(S), and if D1 is set D1 = gelu'(S)
-//   EPI_GRAD  O1 = S * D1 and, with D2, O2 = S * D2
-// H, D1, D2, O1, O2 are [M, ldi] matrices (bf16: rows rounded up to 16; H, O1 and O2 in blocks, D1 and D2 row-major) with
-// n_store (N rounded up to 8) stored columns; those from N on are stored as zeros, so that a later reduction over
-// them in whole 16-byte chunks adds nothing.
-enum { EPI_OUT = 0, EPI_GLU = 1, EPI_GELU = 2, EPI_GRAD = 3 };
-
-// How an operand's element (r, k) lies (see plain.hip): row-major with the reduction contiguous, r * ld + k, fetched a
-// slab (KC) or two (KC2) at a time; row-major with the rows contiguous, k * ld + r (MC); in blocks of 16 x 32
-// with r the token (BK) or k (BM).
-enum { LAY_KC = 0, LAY_KC2 = 1, LAY_MC = 2, LAY_BK = 3, LAY_BM = 4 };
 
 // bf16 activations of this path: element (t, j) of a [T, ldi] matrix.  Blocks of 16 tokens x 32 neurons, 1 KiB each,
 // [token block][neuron block]; in a block the 16-byte chunk c of token r lies at 4 r + (c ^ f(r / 4)), f = 0 2 3 1.

@@ -704,63 +704,6 @@ static int launch_tile(const PlainArgs& a, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-enum { PS_128x128 = 0, PS_256x256 = 1, PS_64x64 = 2, PS_256x128 = 3, PS_SHAPES = 4 };
-struct Plan { int shape, split; };
-
-// Choice of the tile and of the ranges that the reduction is cut into, by estimated time (us): t[k - 1] a slab with k
-// workgroups on a CU, per_cu of which a CU holds at a time, `fixed` for filling the ring and storing.  256 CUs; the
-// fullest one sets the time.  The figures are a least-squares fit to 6800 timings of 460 products (1 to 6000 rows, the
-// layers' widths from 256 to 5120, operands that no cache holds) on every tile and up to 16 ranges; the chosen one
-// takes 1.2 % (bf16) and 0.3 % (fp32) longer than the best on average, 8 % and 2 % in the 95th percentile.  What they
-// show: an XCD's L2 hands its 32 CUs 64 bytes per channel and clock, 64 KB a us and CU, so that two 128x128 tiles (32 KB
-// a slab) take as long as their MFMAs would twice over, and one 256x256 tile as long as its own.
-struct ShapeCost { int bm, bn, per_cu; float t[3], fixed; };
-static const ShapeCost SHAPE_BF16[PS_SHAPES] = {{128, 128, 2, {0.252f, 0.477f}, 2.5f}, {256, 256, 1, {0.547f}, 4.2f},
-                                                {64, 64, 3, {0.144f, 0.276f, 0.449f}, 1.8f}, {256, 128, 1, {0.355f}, 3.0f}};
-static const ShapeCost SHAPE_BF16_GATED64 = {64, 128, 2, {0.203f, 0.433f}, 2.1f};
-static const ShapeCost SHAPE_F32[PS_SHAPES] = {{128, 128, 2, {0.992f, 1.607f}, 1.7f}, {}, {64, 64, 3, {0.324f, 0.588f, 0.919f}, 0.5f}, {}};
-struct ProductCost {
-  float layout[3];        // factor of a slab: right operand turned round, neither, both
-  float bw, overlap;      // bytes a us, and the share of the traffic's time that comes on top
-  float sum, sum_range, sum_bw;   // adding ranges: a launch, each range, bytes a us
-};
-static const ProductCost COST_BF16 = {{1.0f, 1.07f, 1.11f}, 4.91e6f, 0.34f, 1.7f, 0.12f, 2.29e6f};
-static const ProductCost COST_F32 = {{1.0f, 0.99f, 0.99f}, 2.20e6f, 0.22f, 2.0f, 0.10f, 1.70e6f};
-constexpr size_t PART_ROOM = (size_t)64 << 20;   // scratch for ranges' sums
-
-static inline bool turned(int lay) { return lay == LAY_MC || lay == LAY_BM; }
-
-static Plan plain_plan(const PlainArgs& a, int epi, int bf16) {
-  const ProductCost& c = bf16 ? COST_BF16 : COST_F32;
-  const int esz = bf16 ? 2 : 4, planes = epi == EPI_GLU || a.twin ? 2 : 1;
-  const int bk = bf16 ? 32 : 16, slabs = a.segs * ((a.K + bk - 1) / bk);
-  const float layout = c.layout[turned(a.a_lay) ? 2 : turned(a.b_lay) ? 0 : 1];
-  const int stored = epi == EPI_GLU ? 3 : epi == EPI_GELU ? 2 : epi == EPI_GRAD ? (a.D2 ? 4 : 2) : planes;
-  const float bytes = (float)esz * ((float)a.M * a.K * a.segs + (float)a.N * a.K * (planes > a.segs ? planes : a.segs) +
-                                    (float)stored * a.M * a.N);
-  Plan best = {PS_128x128, 1};
-  float best_t = 1e30f;
-  for (int s = 0; s < PS_SHAPES; ++s) {
-    const ShapeCost& q = !bf16 ? SHAPE_F32[s] : s == PS_64x64 && epi == EPI_GLU ? SHAPE_BF16_GATED64 : SHAPE_BF16[s];
-    if (q.bm == 0) continue;
-    const int bn = epi == EPI_GLU ? q.bn / 2 : q.bn;
-    const int64_t tiles = (int64_t)((a.M + q.bm - 1) / q.bm) * ((a.n_store + bn - 1) / bn) * (a.twin ? 2 : 1);
-    for (int split = 1; split <= 16; split += split < 4 ? 1 : split < 8 ? 2 : 4) {
-      const size_t part = (size_t)split * planes * a.M * a.n_store * 4;
-      if (split > 1 && (part > PART_ROOM || tiles * split > 1024 || slabs / split < 4)) break;
-      const int n = (slabs + split - 1) / split;
-      const int64_t load = (tiles * split + 255) / 256, full = load / q.per_cu, rest = load % q.per_cu;
-      float t = (float)full * (n * q.t[q.per_cu - 1] * layout + q.fixed);
-      if (rest) t += n * q.t[rest - 1] * layout + q.fixed;
-      t += c.overlap * bytes / c.bw;
-      if (t < bytes / c.bw) t = bytes / c.bw;
-      if (split > 1) t += c.sum + c.sum_range * split + (float)part / c.sum_bw;
-      if (t < best_t) { best_t = t; best.shape = s; best.split = split; }
-    }
-  }
-  return best;
-}
-
 template <typename T, int LA_, int LB_, int EPI>
 static int launch_shape(const PlainArgs& a, int shape, hipStream_t st) {
   constexpr bool BF = sizeof(T) == 2, PAIRED = LA_ == LAY_KC2 || LB_ == LAY_KC2;
@@ -819,14 +762,18 @@ static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) 
   return -1;
 }
 
-size_t plain_part_room() { return PART_ROOM; }
+size_t plain_part_room() { return PLAIN_PART_ROOM; }
+
+static PlainShape shape_of(const PlainArgs& a, int epi) {
+  return {a.M, a.N, a.K, a.segs, a.twin, epi, a.D2 != nullptr, turned(a.a_lay), turned(a.b_lay)};
+}
 
 int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st) {
   if (a.M <= 0 || a.N <= 0) return 0;
   if ((a.lda & 7) || (a.ldb & 7) || (a.segs != 1 && a.segs != 2) || a.n_store < a.N) return -1;
   // a lane's offset inside a tile stays below 2 GiB
   if (a.lda > (1 << 20) || a.ldb > (1 << 20)) return -1;
-  const Plan pl = plain_plan(a, epi, bf16);
+  const PlainPlan pl = plain_plan(shape_of(a, epi), bf16);
   a.n_split = pl.split;
   a.part = pl.split > 1 ? part : nullptr;
   a.ldp = a.n_store;

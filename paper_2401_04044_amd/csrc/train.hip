@@ -75,10 +75,11 @@ int aligned_weights(const Dense& s, const void* W1, const void* Wg, char* ws, co
   return launch_pad_rows(W1, s.gated ? Wg : nullptr, ws, ws + s.pad_bytes, s.d, s.f, s.bf16, st);
 }
 
-PlainArgs product(int64_t M, int N, int64_t K) {
+PlainArgs product(const Dense& s, int which, int planes) {
+  const PlainShape q = dense_product(which, s.T, s.d, s.f, planes);
   PlainArgs a = {};
-  a.M = (int)M; a.N = N; a.K = (int)K; a.n_store = round_up(N, 8);
-  a.segs = 1;
+  a.M = (int)q.M; a.N = (int)q.N; a.K = (int)q.K; a.n_store = round_up((int)q.N, 8);
+  a.segs = q.segs; a.twin = q.twin;
   a.a_lay = LAY_KC2; a.b_lay = LAY_MC;
   return a;
 }
@@ -98,13 +99,13 @@ int dense_forward(const Dense& s, const void* X, const void* W1, const void* Wg,
   char* const H = kept ? (char*)kept : at;
   if (!kept) at += s.act_bytes;
   float* const part = (float*)at;
-  PlainArgs a = product(s.T, s.f, s.d);
+  PlainArgs a = product(s, DENSE_UP, s.planes);
   a.A[0] = X; a.lda = s.d; a.a_bytes = extent(s.T, s.d, s.d, s.esz);
   a.B[0] = s.gated ? g : u; a.B[1] = u; a.ldb = s.f8; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
   a.H = H; a.ldi = s.ldi;
   if (kept) { a.D1 = H + s.act_bytes; a.D2 = H + 2 * s.act_bytes; }
   if (launch_plain(a, s.gated ? EPI_GLU : EPI_GELU, s.bf16, part, st)) return -1;
-  a = product(s.T, s.d, s.f);
+  a = product(s, DENSE_DOWN, s.planes);
   a.A[0] = H; a.lda = s.ldi; a.a_lay = act_k(s); a.a_bytes = act_extent(s);
   a.B[0] = W2; a.ldb = s.d; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
   a.C[0] = Y; a.ldc = s.d; a.resid = residual; a.out_f32 = y_f32;
@@ -126,7 +127,7 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   PlainArgs a;
   if (dX || dW1 || dWg) {
     // dU = (dY W2^T) D1, dG = (dY W2^T) D2
-    a = product(s.T, s.f, s.d);
+    a = product(s, DENSE_GRAD, s.planes);
     a.A[0] = dY; a.lda = s.d; a.a_bytes = x_ext;
     a.B[0] = W2; a.ldb = s.d; a.b_lay = LAY_KC; a.b_bytes = extent(s.f, s.d, s.d, s.esz);
     a.D1 = H + s.act_bytes; a.O1 = dU; a.ldi = s.ldi;
@@ -135,26 +136,24 @@ int dense_backward(const Dense& s, const void* X, const void* W1, const void* Wg
   }
   if (dX) {
     // dX = dU W1^T + dG Wg^T
-    a = product(s.T, s.d, s.f);
+    a = product(s, DENSE_DX, s.planes);
     a.A[0] = dU; a.A[1] = dG; a.lda = s.ldi; a.a_lay = act_k(s); a.a_bytes = act_ext;
     a.B[0] = u; a.B[1] = g; a.ldb = s.f8; a.b_lay = s.bf16 ? LAY_KC2 : LAY_KC; a.b_bytes = extent(s.d, s.f8, s.f8, s.esz);
-    a.segs = s.planes;
     a.C[0] = dX; a.ldc = s.d;
     if (launch_plain(a, EPI_OUT, s.bf16, part, st)) return -1;
   }
   if (dW1 || dWg) {
     // dW1 = X^T dU, dWg = X^T dG: one launch if both are wanted
-    a = product(s.d, s.f, s.T);
+    a = product(s, DENSE_DUP, dW1 && dWg ? 2 : 1);
     a.A[0] = X; a.lda = s.d; a.a_lay = LAY_MC; a.a_bytes = x_ext;
     a.B[0] = dW1 ? dU : dG; a.B[1] = dG; a.ldb = s.ldi; a.b_lay = act_m(s); a.b_bytes = act_ext;
     a.C[0] = dW1 ? dW1 : dWg; a.C[1] = dWg; a.ldc = s.f;
-    a.twin = dW1 && dWg;
     a.out_f32 = grad_f32; a.accumulate = accumulate;
     if (launch_plain(a, EPI_OUT, s.bf16, part, st)) return -1;
   }
   if (dW2) {
     // dW2 = H^T dY
-    a = product(s.f, s.d, s.T);
+    a = product(s, DENSE_DDOWN, s.planes);
     a.A[0] = H; a.lda = s.ldi; a.a_lay = act_m(s); a.a_bytes = act_ext;
     a.B[0] = dY; a.ldb = s.d; a.b_lay = LAY_MC; a.b_bytes = x_ext;
     a.C[0] = dW2; a.ldc = s.d;

@@ -146,3 +146,14 @@ def test_clipping_by_a_factor_below_the_normal_numbers(ff, limit, dtype):
     # in two halves, into other buffers: the same bits
     two = ff.grad_clip([g[:2048], g[2048:]], norm, limit, out=[torch.empty_like(g[:2048]), torch.empty_like(g[2048:])])
     assert torch.equal(torch.cat(two), out)
+
+
+def test_silu_in_fp32_neuron_by_neuron(ff):
+    """An exponential, a division and two products: 16 half steps of the value, of 1 + |z| for the slope (which has a zero)."""
+    z = np.linspace(-80, 40, 256).astype(np.float32).astype(np.float64)
+    H, dU, dG = _one_to_one(ff, "swiglu", "f32", z, np.ones(256))
+    s = 1 / (1 + np.exp(-z))
+    assert (np.abs(H - z * s) <= 16 * 2.0 ** -24 * np.abs(z * s)).all()
+    assert (np.abs(dU - z * s) <= 16 * 2.0 ** -24 * np.abs(z * s)).all()
+    slope = s * (1 + z * (1 - s))
+    assert (np.abs(dG - slope) <= 16 * 2.0 ** -24 * s * (1 + np.abs(z))).all()

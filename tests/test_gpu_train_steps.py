@@ -45,3 +45,62 @@ def test_micro_batches_take_the_norm_once(ff, dtype):
     want = ff.grad_clip([t[k] for t in total for k in t], norm, limit)
     assert int(flag) == 0 and abs(float(norm) - 2 * limit) <= 2.0 ** -22 * limit
     assert all(torch.equal(a, w) for a, w in zip([a[k] for a in acc for k in a], want))
+
+
+@pytest.mark.parametrize("dtype,T,d,f,act", [("bf16", 300, 512, 1365, "swiglu"), ("bf16", 1030, 1024, 2816, "swiglu"),
+                                             ("bf16", 700, 1280, 5120, "gelu"), ("f32", 513, 768, 2048, "gelu")])
+def test_a_stack_of_ordinary_width_is_its_parts(ff, dtype, T, d, f, act):
+    """Three layers: what the driver gives is what the single calls give, bit for bit (which other tests hold to 64 bits)."""
+    import train_ref as tr
+    n, gen = 3, torch.Generator(device="cuda")
+    gen.manual_seed(T + d)
+    desc = ff.make_desc(d, f, act, dtype)
+    layers = [dict(zip(("W1", "Wg", "W2"), tr.make_layer(gen, d, f, act == "swiglu", 1, dtype)[1:4])) for _ in range(n)]
+    x0 = torch.randn(T, d, generator=gen, device="cuda")
+    dy = torch.randn(T, d, generator=gen, device="cuda") * 1e-3
+    x, dx = x0.clone(), dy.clone()
+    saved = ff.dense_stack_forward(desc, layers, x, want_saved=True)
+    grads, norm, flag = ff.dense_stack_backward(desc, layers, saved, dx, max_norm=1e-2)
+    kind, dt = (ff.BF16, torch.bfloat16) if dtype == "bf16" else (ff.F32, torch.float32)
+    y, tape = x0.clone(), []
+    for W in layers:
+        m = ff.token_rmsnorm(y, kind)
+        out, kept = ff.dense_forward(desc, m, W["W1"], W["Wg"], W["W2"], residual=y, y_f32=True, want_saved=True)
+        tape.append((y, m, kept))
+        y = out
+    assert torch.equal(x, y)
+    g, own = dy.clone(), [None] * n
+    for l in reversed(range(n)):
+        W, (xi, m, kept) = layers[l], tape[l]
+        dn, own[l] = ff.dense_backward(desc, m, W["W1"], W["Wg"], W["W2"], kept, g.to(dt))
+        g = ff.token_rmsnorm_backward(xi, dn, residual=g)
+    assert torch.equal(dx, g)
+    # (the driver adds the squares matrix by matrix, W2 before Wg: the norm is the same to a step)
+    flat = [own[l][k] for l in range(n) for k in ("W1", "Wg", "W2") if own[l][k] is not None]
+    n1, f1 = ff.grad_norm(flat)
+    assert int(flag) == int(f1) == 0 and abs(float(norm) - float(n1)) <= 2.0 ** -23 * float(n1)
+    clipped = ff.grad_clip(flat, norm, 1e-2)
+    assert all(torch.equal(a, b) for a, b in zip([grads[l][k] for l in range(n) for k in ("W1", "Wg", "W2") if grads[l][k] is not None], clipped))
+
+
+@pytest.mark.parametrize("act", ["swiglu", "gelu"])
+def test_a_bf16_stack_of_ordinary_width_against_the_oracle(ff, act):
+    T, d, f, n = 200, 512, 1365, 2
+    rng = np.random.default_rng(60)
+    hosts = [tu.make_layer(rng, d, f, act == "swiglu", T, "bf16") for _ in range(n)]
+    layers = [h[1:4] for h in hosts]
+    x0, dy = hosts[0][0], rng.standard_normal((T, d)).astype(np.float32)
+    desc = ff.make_desc(d, f, act, "bf16")
+    dev = [dict(zip(("W1", "Wg", "W2"), tu.to_dev(W, "bf16"))) for W in layers]
+    x, dx = torch.from_numpy(x0).cuda(), torch.from_numpy(dy).cuda()
+    saved = ff.dense_stack_forward(desc, dev, x, want_saved=True)
+    grads, norm, flag = ff.dense_stack_backward(desc, dev, saved, dx)
+    wx, tape = orc.stack_forward(layers, x0, EPS)
+    wdx, wg = orc.stack_backward(layers, tape, dy, EPS)
+    # a layer and its norm round about ten times by at most 2^-8 on the way down and up: one layer's bar for each
+    tol = n * gu.TOL["bf16"]
+    assert gu.relf(gu.host(x), wx) < tol and gu.relf(gu.host(dx), wdx) < tol and int(flag) == 0
+    for l in range(n):
+        for k in wg[l]:
+            if wg[l][k] is not None:
+                assert gu.relf(gu.host(grads[l][k]), wg[l][k]) < tol, (l, k)
