@@ -405,7 +405,8 @@ int ffsplit_dense_stack_forward(const ffsplit_desc_t* desc, int32_t n_layers, co
  * that receive the weights' gradients (flags as for ffsplit_dense_backward).  If norm is not NULL the norm
  * over all of them goes to *norm and *nonfinite (ffsplit_grad_norm; nonfinite may be NULL), and if also
  * max_norm > 0 they are clipped in place (ffsplit_grad_clip; 0 or less: not; NaN is refused).
- * workspace: as for the forward pass.
+ * workspace: as for the forward pass (beyond 4096 layers, with the norm, at least
+ * ffsplit_workspace_bytes(NULL, FFSPLIT_WS_GRAD_NORM, 3 n_layers)).
  */
 int ffsplit_dense_stack_backward(const ffsplit_desc_t* desc, int32_t n_layers, const void* const* W1,
                                  const void* const* Wg, const void* const* W2, const void* kept, float* dx,

@@ -46,9 +46,7 @@ struct PlainArgs {
   int group_m;   // row tiles per rasterisation group (set by the launcher)
 };
 
-// Bytes of scratch that hold the ranges' sums of any product (see plain_plan).
-size_t plain_part_room();
-// part: that many bytes
+// part: scratch of plain_part_bytes() of this product
 int launch_plain(PlainArgs a, int epi, int bf16, float* part, hipStream_t st);
 // dst[r][0 .. cols8) = src[r][0 .. cols), zeros behind, of one or two matrices; cols8 = cols rounded up to 8; rows a
 // multiple of 8

@@ -762,8 +762,6 @@ static int launch_typed(const PlainArgs& a, int epi, int shape, hipStream_t st) 
   return -1;
 }
 
-size_t plain_part_room() { return PLAIN_PART_ROOM; }
-
 static PlainShape shape_of(const PlainArgs& a, int epi) {
   return {a.M, a.N, a.K, a.segs, a.twin, epi, a.D2 != nullptr, turned(a.a_lay), turned(a.b_lay)};
 }

@@ -67,6 +67,17 @@ struct ProductCost {
 static const ProductCost COST_BF16 = {{1.0f, 1.07f, 1.11f}, 4.91e6f, 0.34f, 1.7f, 0.12f, 2.29e6f};
 static const ProductCost COST_F32 = {{1.0f, 0.99f, 0.99f}, 2.20e6f, 0.22f, 2.0f, 0.10f, 1.70e6f};
 constexpr size_t PLAIN_PART_ROOM = (size_t)64 << 20;   // scratch for ranges' sums, at most
+constexpr int PLAIN_MAX_SPLIT = 16, PLAIN_MIN_SLABS = 4;   // ranges, and slabs of each
+
+// Scratch for the ranges' sums of a product, whatever is chosen for it: as many ranges as its slabs allow, never less for a
+// longer side.
+inline size_t plain_part_bytes(const PlainShape& a, int bf16) {
+  const int64_t bk = bf16 ? 32 : 16, most = a.segs * ((a.K + bk - 1) / bk) / PLAIN_MIN_SLABS;
+  if (most < 2) return 0;
+  const size_t bytes = (size_t)(most < PLAIN_MAX_SPLIT ? most : PLAIN_MAX_SPLIT) * (a.epi == EPI_GLU || a.twin ? 2 : 1) * a.M *
+                       ((a.N + 7) / 8 * 8) * 4;
+  return bytes < PLAIN_PART_ROOM ? bytes : PLAIN_PART_ROOM;
+}
 
 inline PlainPlan plain_plan(const PlainShape& a, int bf16) {
   const ProductCost& c = bf16 ? COST_BF16 : COST_F32;
@@ -83,9 +94,9 @@ inline PlainPlan plain_plan(const PlainShape& a, int bf16) {
     if (q.bm == 0) continue;
     const int bn = a.epi == EPI_GLU ? q.bn / 2 : q.bn;
     const int64_t tiles = ((a.M + q.bm - 1) / q.bm) * ((n_store + bn - 1) / bn) * (a.twin ? 2 : 1);
-    for (int split = 1; split <= 16; split += split < 4 ? 1 : split < 8 ? 2 : 4) {
+    for (int split = 1; split <= PLAIN_MAX_SPLIT; split += split < 4 ? 1 : split < 8 ? 2 : 4) {
       const size_t part = (size_t)split * planes * a.M * n_store * 4;
-      if (split > 1 && (part > PLAIN_PART_ROOM || tiles * split > 1024 || slabs / split < 4)) break;
+      if (split > 1 && (part > PLAIN_PART_ROOM || tiles * split > 1024 || slabs / split < PLAIN_MIN_SLABS)) break;
       const int n = (int)((slabs + split - 1) / split);
       const int64_t load = (tiles * split + 255) / 256, full = load / q.round, rest = load % q.round;
       float t = (float)full * (n * q.t[q.round - 1] * layout + q.fixed);

@@ -56,13 +56,22 @@ Dense dense_of(const ffsplit_desc_t& d, int64_t T) {
   return s;
 }
 
+// scratch for the ranges' sums of any of a pass's products, one after the other
+size_t part_room(const Dense& s, int first, int last) {
+  size_t room = 0;
+  for (int which = first; which <= last; ++which) {
+    const size_t n = plain_part_bytes(dense_product(which, s.T, s.d, s.f, s.planes), s.bf16);
+    if (n > room) room = n;
+  }
+  return align256(room);
+}
 size_t forward_ws(const ffsplit_desc_t& d, int64_t T) {
   const Dense s = dense_of(d, T);
-  return s.planes * s.pad_bytes + s.act_bytes + plain_part_room();
+  return s.planes * s.pad_bytes + s.act_bytes + part_room(s, DENSE_UP, DENSE_DOWN);
 }
 size_t backward_ws(const ffsplit_desc_t& d, int64_t T) {
   const Dense s = dense_of(d, T);
-  return s.planes * s.pad_bytes + s.planes * s.act_bytes + plain_part_room();
+  return s.planes * s.pad_bytes + s.planes * s.act_bytes + part_room(s, DENSE_GRAD, DENSE_DDOWN);
 }
 size_t kept_bytes(const Dense& s) { return (1 + s.planes) * s.act_bytes; }
 
@@ -173,10 +182,14 @@ StackKept stack_kept(const Dense& s) {
   return k;
 }
 // Scratch of the stack's two passes: normalised tokens (forward without kept state) or the two gradients
-// between a layer and its norm, then the layer's own.
+// between a layer and its norm, then the layer's own.  The norm's sums lie in the same place behind them: room for those of
+// NORM_LAYERS layers whatever the layers' size (4.3 MB).
+constexpr int64_t NORM_LAYERS = 4096;
 size_t stack_ws(const ffsplit_desc_t& d, int64_t T) {
   const Dense s = dense_of(d, T);
-  return 2 * align256((size_t)T * s.d * s.esz) + (forward_ws(d, T) > backward_ws(d, T) ? forward_ws(d, T) : backward_ws(d, T));
+  const size_t f = forward_ws(d, T), b = backward_ws(d, T), n = align256(grad_norm_ws_bytes(3 * NORM_LAYERS));
+  const size_t layers = 2 * align256((size_t)T * s.d * s.esz) + (f > b ? f : b);
+  return layers > n ? layers : n;
 }
 
 }  // namespace

@@ -26,19 +26,22 @@ def plan(tmp_path_factory):
                    '  const auto p = ffsplit::plain_plan(s, bf16);\n'
                    '  out[0] = p.shape; out[1] = p.split; out[2] = s.M; out[3] = s.N; out[4] = s.K; out[5] = s.segs;\n'
                    '  out[6] = s.twin || s.epi == ffsplit::EPI_GLU ? 2 : 1; }\n'
-                   'extern "C" size_t room() { return ffsplit::PLAIN_PART_ROOM; }\n')
+                   'extern "C" size_t room() { return ffsplit::PLAIN_PART_ROOM; }\n'
+                   'extern "C" size_t bytes(int which, long T, int d, int f, int planes, int bf16) {\n'
+                   '  return ffsplit::plain_part_bytes(ffsplit::dense_product(which, T, d, f, planes), bf16); }\n')
     subprocess.check_call(["g++", "-std=c++17", "-O2", "-shared", "-fPIC",
                            "-I" + os.path.join(ROOT, "paper_2401_04044_amd", "csrc"), str(src), "-o", str(so)])
     lib = ctypes.CDLL(str(so))
     lib.plan.argtypes = [ctypes.c_int, ctypes.c_long] + [ctypes.c_int] * 4 + [ctypes.POINTER(ctypes.c_long)]
     lib.room.restype = ctypes.c_size_t
+    lib.bytes.argtypes, lib.bytes.restype = [ctypes.c_int, ctypes.c_long] + [ctypes.c_int] * 4, ctypes.c_size_t
 
     def get(which, T, d, f, planes, bf16):
         out = (ctypes.c_long * 7)()
         lib.plan(which, T, d, f, planes, bf16, out)
         return list(out)
 
-    get.room = lib.room()
+    get.room, get.bytes = lib.room(), lib.bytes
     return get
 
 
@@ -90,7 +93,7 @@ def test_ranges_fit_their_scratch_and_are_worth_it(plan):
             assert 1 <= split <= 16
             if split > 1:
                 cut += 1
-                assert split * outs * M * (N + 7) // 8 * 8 * 4 <= plan.room
+                assert split * outs * M * (-(-N // 8) * 8) * 4 <= plan.room
                 assert segs * -(-K // (32 if bf16 else 16)) // split >= 4
     assert cut > 1000
 
@@ -105,3 +108,30 @@ def test_the_products_of_the_two_passes(plan):
             assert tuple(got[2:5]) == (M, N, K)
             assert got[5] == (planes if which == DX else 1)
             assert got[6] == (planes if which in (UP, DUP) else 1)
+
+
+def test_the_scratch_holds_what_is_chosen(plan):
+    """Of a product, and of each with one gradient of a gated layer alone: never more than the sized scratch."""
+    rng = np.random.default_rng(13)
+    sizes = list(_sizes(rng, 6000)) + SIZES + [((1 << 28), 8, 8, True, "bf16"), (1, 8, 8, True, "bf16"), (40, 1 << 20, 200, True, "bf16")]
+    for T, d, f, gated, dtype in sizes:
+        bf16 = dtype == "bf16"
+        for which in range(6):
+            room = plan.bytes(which, T, d, f, 1 + gated, bf16)
+            assert room <= plan.room and room <= plan.bytes(which, 2 * T, d, f, 1 + gated, bf16)
+            for planes in {1 + gated, 1} if which == DUP else {1 + gated}:
+                shape, split, M, N, K, segs, outs = plan(which, T, d, f, planes, bf16)
+                if split > 1:
+                    assert split * outs * M * (-(-N // 8) * 8) * 4 <= room, (which, T, d, f, planes, dtype)
+    assert plan.bytes(DUP, 100, 8, 8, 2, True) == 0      # (a reduction that is too short to cut)
+
+
+def test_small_layers_take_small_scratch():
+    import paper_2401_04044_amd as ff
+    desc = ff.make_desc(8, 8, "swiglu", "bf16")
+    for call in (ff.WS_DENSE_FORWARD, ff.WS_DENSE_BACKWARD):
+        assert 0 < ff.workspace_bytes(desc, call, 1) <= 1 << 16
+    # (a stack's holds its norm's sums too, of up to 4096 layers)
+    assert ff.lib.ffsplit_workspace_bytes(None, ff.WS_GRAD_NORM, 3 * 4096) <= ff.workspace_bytes(desc, ff.WS_DENSE_STACK, 1) <= 1 << 23
+    large = ff.make_desc(4096, 11008, "swiglu", "bf16")
+    assert ff.workspace_bytes(large, ff.WS_DENSE_FORWARD, 4096) <= 4096 * 11008 * 2 + (64 << 20)
