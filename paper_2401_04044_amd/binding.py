@@ -496,13 +496,13 @@ class _GradList:
             ptrs.append(g.data_ptr())
             counts.append(g.numel())
             dtypes.append(F32 if dt == torch.float32 else BF16)
-        self._read = set(ptrs)
+        self._at = ptrs if 0 not in counts else [p if c else 0 for p, c in zip(ptrs, counts)]   # 0: nothing there
         self.ptrs, self.counts = (ctypes.c_void_p * max(n, 1))(*ptrs), (ctypes.c_int64 * max(n, 1))(*counts)
         self.dtypes = (ctypes.c_int32 * max(n, 1))(*dtypes)
 
     def out_ptrs(self, grads, out):
         if out is None:
-            self._apart(self.ptrs)
+            self._apart(self._at)
             return self.ptrs
         if len(out) != self.n:
             raise ValueError(f"out: {len(out)} tensors for {self.n} gradients")
@@ -511,15 +511,18 @@ class _GradList:
             if o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous() or o.device != self.device:
                 raise ValueError("out: tensors like the gradients are wanted, contiguous and on their device")
             ptrs.append(o.data_ptr())
-        self._apart(ptrs)
-        if not self._read.isdisjoint(ptrs) and any(p in self._read and p != q for p, q, c in zip(ptrs, self.ptrs, self.counts) if c):
+        at = ptrs if self._at.count(0) == 0 else [p if q else 0 for p, q in zip(ptrs, self._at)]
+        there = self._apart(at)
+        if not there.isdisjoint(self._at) and any(p != q and p in there for p, q in zip(self._at, at) if p):
             raise ValueError("out: the buffer of another gradient, which is still read")
         return (ctypes.c_void_p * max(self.n, 1))(*ptrs)
 
-    def _apart(self, ptrs):
-        written = [p for p, c in zip(ptrs, self.counts) if c]
-        if len(set(written)) != len(written):
+    def _apart(self, at):
+        there = set(at)
+        if len(there) + max(at.count(0) - 1, 0) != len(at):
             raise ValueError("gradients: a tensor that is written is listed twice")
+        there.discard(0)
+        return there
 
     def norm(self, norm, flag, workspace):
         dev = self.device
