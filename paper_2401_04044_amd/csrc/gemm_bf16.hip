@@ -33,6 +33,7 @@
 // Epilogues: plain / GeLU / SwiGLU (on (gate, up) pairs of 32-column blocks)
 // with two output destinations, fp32 split-K partials, and the neuron-norm
 // column reduction of Sec. 4.1 (Eq. 3) for the calibration pass.
+#include "wave.h"
 #include "common.h"
 #include <atomic>
 #include <algorithm>
@@ -49,11 +50,6 @@ union Frag {
   u32x4_t u;
   bf16x8_t v;
 };
-
-__device__ __forceinline__ int xcd_remap(int i, int total) {
-  const int q = total >> 3, rem = total & 7, x = i & 7;
-  return x * q + (x < rem ? x : rem) + (i >> 3);
-}
 
 template <int ACT>
 __device__ __forceinline__ float act_bf16(float z, float g) {
@@ -229,21 +225,6 @@ __device__ __forceinline__ void buffer_to_lds(const void* base, lptr_t dst, uint
   __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, -1, 0x00027000), dst, 16,
                                            lane_off, scalar_off, 0, 0);
 }
-
-// s_waitcnt with only the vector-memory counter constrained (gfx9 encoding: vmcnt in
-// imm[3:0] and imm[15:14], expcnt imm[6:4], lgkmcnt imm[11:8])
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
-}
-template <int N>
-__device__ __forceinline__ void wait_lgkmcnt() {
-  __builtin_amdgcn_s_waitcnt(0xc07f | ((N < 15 ? N : 15) << 8));
-}
-// workgroup barrier without a memory fence (the kernel orders its loads with explicit counters);
-// the memory clobber keeps the compiler from moving LDS accesses across it
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
-#define FFS_ORDER __builtin_amdgcn_sched_barrier(0)   // instructions keep the written order
 
 // The accumulators of a tile's ranges (blockIdx.y) added by the last workgroup to arrive, which gets them in
 // acc and true; the others are done.  The XCDs' L2 caches are not coherent within a launch: device-scope

@@ -15,6 +15,7 @@
 // 1280 tokens 186 -> 173, 2048 266 -> 249, 4096 449 -> 425; rank 256, 6000 tokens 314 -> 288;
 // 5120 x 13824, rank 1280, 4096 tokens 625 -> 601.  Issuing all its loads right behind that barrier
 // was slower still.
+#include "wave.h"
 #include "common.h"
 #include <atomic>
 #include <type_traits>
@@ -42,10 +43,6 @@ constexpr int DLA = DA_BLK / DNW, DLPW = DLA + DB_BLK / DNW;          // loads p
 constexpr int DSTAGE = (DA_BLK + DB_BLK) * 64;                        // 16-byte chunks of a stage
 static_assert(DA_BLK % DNW == 0 && DB_BLK % DNW == 0 && DSTAGES * DLPW <= 63, "loads of a slab");
 
-template <int N>
-__device__ __forceinline__ void dual_wait_vmcnt() {   // gfx9 encoding, as in gemm_bf16.hip
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
-}
 __device__ __forceinline__ void dual_swap32(uint32_t& a, uint32_t& b) {
   auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
   a = r[0];
@@ -136,12 +133,12 @@ gemm_dual_kernel(const GemmArgs p) {
   // slab s has landed once at most the loads of the slabs issued after it (up to `last`) are outstanding
   auto wait_landed = [&](int s, int last, auto full) {
     if (decltype(full)::value) {
-      dual_wait_vmcnt<(DSTAGES - 2) * DLPW>();
+      wait_vmcnt<(DSTAGES - 2) * DLPW>();
     } else {
       const int later = min(nk - 1, last) - s;
-      if (later <= 0) dual_wait_vmcnt<0>();
-      else if (later == 1) dual_wait_vmcnt<DLPW>();
-      else dual_wait_vmcnt<2 * DLPW>();
+      if (later <= 0) wait_vmcnt<0>();
+      else if (later == 1) wait_vmcnt<DLPW>();
+      else wait_vmcnt<2 * DLPW>();
     }
   };
 

@@ -24,6 +24,7 @@
 // The buffers' bounds are exact: what lies behind an operand's end reads as zero, which is how a
 // reduction that ends inside a slab and rows behind the last are handled, without masks in the loop.
 #include "plain_epi.h"
+#include "wave.h"
 #include <atomic>
 #include <algorithm>
 #include <math.h>
@@ -42,23 +43,6 @@ union Frag {
   f32x4_t f;
 };
 
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
-}
-template <int N>
-__device__ __forceinline__ void wait_lgkmcnt() {
-  __builtin_amdgcn_s_waitcnt(0xc07f | ((N < 15 ? N : 15) << 8));
-}
-// workgroup barrier without a memory fence (the kernel orders its loads with explicit counters)
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-#define FFS_ORDER __builtin_amdgcn_sched_barrier(0)   // instructions keep the written order
-
-__device__ __forceinline__ int xcd_remap(int i, int total) {
-  const int q = total >> 3, rem = total & 7, x = i & 7;
-  return x * q + (x < rem ? x : rem) + (i >> 3);
-}
 __device__ __forceinline__ uint32_t kc_swizzle(uint32_t r4) { return (0x78u >> (2 * (r4 & 3))) & 3; }   // 0 2 3 1
 
 constexpr uint32_t NOWHERE = 0x80000000u;   // beyond every resource's end
