@@ -12,9 +12,9 @@ namespace {
 // n = r x with r = (mean(x^2) + eps)^(-1/2), so dx = r (dn - (r x) (r mean(x dn))): two sums over the row,
 // then one pass.  (r x is of order one and r mean(x dn) of the order of dn, so that the gradient is right wherever n
 // is; r^3 alone leaves fp32 for tokens of 1e13 or 1e-13.)
-// TPR threads per row, which keep it in registers (one read of everything): rows of up to
-// 1024 elements in a wavefront, 8192 in a workgroup, where longer ones are read a second time.  5120 rows of 4096, bf16 with residual and copy, 294 MB: 48 us
-// (6.1 TB/s) in traces, 56 a call back to back.
+// TPR threads per row, which keep it in registers (one read of everything): rows of up to 1024 elements in a wavefront,
+// 8192 in a workgroup, where longer ones are read a second time.  4096 rows of 5120, bf16 with the residual, 294 MB: 49 us
+// (6.0 TB/s) in traces, 50 to 56 a call back to back.
 template <bool BF16, int TPR>
 __global__ void __launch_bounds__(256) rmsnorm_backward_kernel(const float* x, const void* dn, int64_t T, int d, float eps,
                                                                const float* residual, float* dx, void* cast) {
