@@ -615,7 +615,7 @@ def dense_stack_backward(desc, layers, saved, dx, eps=1e-6, grads=None, accumula
         raise ValueError("gradients: a buffer is listed twice")
     if grads is not None:
         _grads_apart([t for q in g for t in q.values() if t is not None],
-                     [t for W in layers for t in W.values() if t is not None] + [saved, dx])
+                     [W[k] for W in layers for k in ("W1", "Wg", "W2") if W.get(k) is not None] + [saved, dx])
     if max_norm > 0 and not want_norm:
         raise ValueError("max_norm: clipping needs the norm")
     W1, Wg, W2 = _stack_args(desc, layers, dev)

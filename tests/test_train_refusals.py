@@ -96,3 +96,13 @@ def test_clipping_without_the_norm_is_refused():
     saved = torch.zeros(1 << 20, dtype=torch.uint8)
     with pytest.raises(ValueError, match="needs the norm"):
         ff.dense_stack_backward(desc, [{"W1": t["W1"], "W2": t["W2"]}], saved, t["dY"], max_norm=1.0, want_norm=False)
+
+
+def test_layers_may_carry_more_than_their_weights():
+    """A program's layer dicts hold other things as well: the stack's calls look at W1, Wg and W2."""
+    desc, t = _layer(T=4, act="gelu")
+    layers = [{"W1": t["W1"], "W2": t["W2"], "Wg": None, "name": "ffn.0", "steps": 3}]
+    grads = [{"W1": torch.zeros_like(t["W1"]), "W2": torch.zeros_like(t["W2"])}]
+    saved = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="GPU"):
+        ff.dense_stack_backward(desc, layers, saved, t["dY"], grads=grads)
